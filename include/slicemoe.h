@@ -162,6 +162,27 @@ int smoe_route(smoe_ctx* ctx, int T, int E, int k, int d_model, const float* log
                int norm_topk, float routed_scale, float* logits_out_dev, int32_t* idx_dev,
                float* w_dev);
 
+/* Routing as the later mixture-of-experts models do it: a choice by score + bias, over groups first.  z as in smoe_route
+ * (logits_dev fp32 [T,E], or the product of w_router_dev and x_dev).  s_e = sigmoid(z_e) or softmax(z)_e; c_e = s_e +
+ * bias_e (bias_dev fp32 [E] or NULL = 0: a balance bias, a cache boost, or their sum).  The E / n_group experts of a group
+ * are neighbours; a group's score is its largest c_e (SMOE_GROUP_MAX) or the sum of its two largest (SMOE_GROUP_TOP2; the
+ * largest where the group has one expert), and the topk_group best groups stay.  idx_dev[t,0..k) = the k largest c_e in
+ * them from the highest down; equal scores go to the lower group and the lower expert.  w_dev[t,j] = s of the chosen
+ * expert, divided by the sum of the chosen ones if norm_topk, times routed_scale.  Scores, sums and comparisons are
+ * binary64, weights are rounded to fp32 once.
+ *   A logit of minus infinity scores 0 (a masked expert: chosen only where nothing else is left); a token without any
+ * other logit gets weights 0.  A NaN ranks below every number: with softmax it makes the token's weights NaN, with sigmoid
+ * the expert's own (and with norm_topk those beside it).
+ * E <= 256, k <= 16, n_group <= 64 and a divisor of E, k <= topk_group * E / n_group, T <= 2^22 (SMOE_ESHAPE).  With the
+ * mat-vec the activations of a token stand in LDS: SMOE_ESIZE above 64 KiB (d_model about 28000 in bf16 and 14000 in fp32 less
+ * what 12 E bytes take). */
+enum { SMOE_SCORE_SOFTMAX = 0, SMOE_SCORE_SIGMOID = 1 };
+enum { SMOE_GROUP_MAX = 0, SMOE_GROUP_TOP2 = 1 };
+int smoe_route_scores(smoe_ctx* ctx, int T, int E, int k, int d_model, const float* logits_dev, const void* x_dev,
+                      int act_dtype, const float* w_router_dev, int score, int n_group, int topk_group,
+                      int group_score, const float* bias_dev, int norm_topk, float routed_scale, int32_t* idx_dev,
+                      float* w_dev);
+
 /* ---- expert_ffn(mask) (Section 4.1) ------------------------------------------------------- */
 /* One token.  y = sum_j w[j] * FFN_{idx[j]}^{prec[j]}(x) + sum_{shared e} gamma * FFN_e^{HIGH}(x)
  * (+ x if add_residual), FFN(x) = Wd (silu(Wg x) * (Wu x)).
@@ -251,6 +272,54 @@ int smoe_prefill_histogram(smoe_ctx* ctx, const smoe_bank* routed, const smoe_ba
                            const void* shared_gate_w_dev, int add_residual, void* scratch_dev,
                            size_t scratch_bytes, void* y_dev, int32_t* idx_dev, float* w_dev,
                            uint32_t* hist_dev);
+
+/* ---- between two blocks ----------------------------------------------------------------------- */
+/* T rows: b = sum_j slot_w[t,j] * y[t,j] over k slots (weights 1 if slot_w_dev is NULL); b = b / sqrt(mean(b^2) + eps) *
+ * post_w unless post_w_dev is NULL; res_out = res + scale * gate * b; x_out = res_out / sqrt(mean(res_out^2) + eps) * pre_w.
+ * y_dev [T,k,d], post_w_dev, pre_w_dev [d], gate_dev [d] or, with gate_rows = 1, [T,d], x_out_dev [T,d] of act_dtype;
+ * slot_w_dev fp32 [T,k]; res_dev, res_out_dev [T,d] of res_dtype.  Everything is worked out in fp32, and x_out from res_out as it is
+ * before its rounding.  NULL leaves a step out: gate_dev (1), pre_w_dev (1), res_dev (0), res_out_dev or x_out_dev (that
+ * output is not written; one of them is needed), y_dev with k = 0 (the norm of a residual alone; slot_w_dev, post_w_dev
+ * and gate_dev NULL then).  res_out_dev may be res_dev (in place); apart from that the outputs must not overlap the inputs
+ * or one another.  eps must not be negative.  d a multiple of 8 up to 16384, k <= 24, T <= 2^22 (SMOE_ESHAPE). */
+int smoe_residual_norm(smoe_ctx* ctx, int T, int d, int k, const void* y_dev, const float* slot_w_dev,
+                       const void* post_w_dev, const void* gate_dev, int gate_rows, float scale, const void* res_dev,
+                       const void* pre_w_dev, float eps, int act_dtype, int res_dtype, void* res_out_dev,
+                       void* x_out_dev);
+
+/* ---- microscaled 4-bit floats (MXFP4) ----------------------------------------------------------- */
+/* A second weight format beside the AMAT store: 17/32 bytes per weight, no slices, run by the matrix cores as it is stored.
+ * [rows, K] numbers are two arrays: codes uint8 [rows, K/2], two e2m1 codes a byte, the even column in the low nibble
+ * (sign bit, then 0 .5 1 1.5 2 3 4 6), and scales uint8 [rows, K/32], X + 127 for the block's power of two X; byte 255 makes the
+ * block NaN.  K is a multiple of 32.  A matrix of experts is [E, N, K] in the same form, so a checkpoint's arrays can be
+ * used where they lie.
+ *   smoe_mx_quantize: X = floor(log2(max |v| of the block)) - 2 within -127 .. 127, -127 for a block of zeros; codes are v / 2^X to the
+ * nearest e2m1 number, ties to the even code, magnitudes above 6 to 6 (a value is off by at most a quarter of itself or 2^X / 4).  A block with an infinity or NaN gets scale byte
+ * 255 and codes 0.  smoe_mx_dequantize: the numbers that codes and scales stand for, rounded to dst_dtype.
+ * src_dev / dst_dev [rows, K] of the given dtype; rows * K <= 2^34 (SMOE_ESHAPE). */
+int smoe_mx_quantize(smoe_ctx* ctx, long long rows, int K, const void* src_dev, int src_dtype, uint8_t* codes_dev,
+                     uint8_t* scales_dev);
+int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const uint8_t* codes_dev, const uint8_t* scales_dev,
+                       void* dst_dev, int dst_dtype);
+/* Product of T tokens with the experts chosen for each, both quantised: slot (t, j) is
+ * y_dev[t,j] = W[idx[t,j]] x, x the token's row t of [T, K] or, with x_slots = 1, the slot's own row t*k + j of [T*k, K].
+ * W [E,N,K]; idx_dev int32 [T,k] as a router leaves it (the same expert may occur twice; an index outside [0, E)
+ * counts as the nearest expert), or NULL with E = 1 and k = 1: a plain product.  swiglu = 0: y_dev [T,k,N];
+ * swiglu = 1: rows 2i and 2i+1 of W are the gate and the up row of column i and y_dev [T,k,N/2] is silu(gate) * up.
+ * Sums are fp32, y_dev is rounded once to out_dtype.  scratch_dev (smoe_mx_product_bytes; not used and may be NULL where
+ * idx_dev is NULL) belongs to the call until its work is done: calls that may overlap need one each.
+ * N a multiple of 16 up to 2^20, K of 32 up to 65536, N*K < 2^32, the rows of x less than 2^31 bytes of codes, E <= 256, k <= 16,
+ * T*k <= 2^22, T*k*N <= 2^35 (SMOE_ESHAPE). */
+int smoe_mx_product_bytes(int T, int k, int E, size_t* scratch_bytes);
+int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
+                    int k, const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, int x_slots, const int32_t* idx_dev,
+                    int swiglu, int out_dtype, void* scratch_dev, size_t scratch_bytes, void* y_dev);
+/* The same for decode steps of T <= 16 tokens, x_dev [T,K] or [T,k,K] of act_dtype taken as it is (not quantised),
+ * y_dev of act_dtype.  Every product of a weight and an activation is exact before the fp32 sum.  No scratch, one launch.  y_dev must
+ * not overlap x_dev. */
+int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
+                   int k, const void* x_dev, int act_dtype, int x_slots, const int32_t* idx_dev, int swiglu,
+                   void* y_dev);
 
 /* Host only.  Retention order after prefill, hottest first: slice id = ((layer*E + expert) << 1)
  * | is_lsb; every MSB slice before any LSB slice, within a plane by descending count, equal counts

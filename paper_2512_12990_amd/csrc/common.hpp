@@ -85,6 +85,21 @@ struct RouteRec {
     if (_e != hipSuccess) { (ctx)->last_hip = (int)_e; return SMOE_EHIP; } \
   } while (0)
 
+// Makes the context's device current for one call and the caller's device current again after it.
+struct DeviceScope {
+  int before = -1;
+  hipError_t rc;
+  explicit DeviceScope(int device) {
+    rc = hipGetDevice(&before);
+    if (rc == hipSuccess && before != device) rc = hipSetDevice(device);
+    else before = -1;
+  }
+  ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+};
+#define ON_DEVICE_OF(ctx) DeviceScope _scope((ctx)->device); HIPCHK(ctx, _scope.rc)
+
 static inline bool aligned16(const void* p) { return (((uintptr_t)p) & 15u) == 0; }
 
 // ---- device helpers ---------------------------------------------------------------------------
@@ -97,6 +112,13 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
   return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
 }
 
+// two fp32 -> two bf16, to nearest even; infinities and NaN stay what they are
+__device__ __forceinline__ uint32_t pack_bf16_rne(float lo, float hi) {
+  typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+  const bf2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
 template <int ACT> __device__ __forceinline__ float load_act(const void* p, size_t i) {
   if (ACT == SMOE_F32) return ((const float*)p)[i];
   return bf16_bits_to_f32(((const uint16_t*)p)[i]);
@@ -104,6 +126,30 @@ template <int ACT> __device__ __forceinline__ float load_act(const void* p, size
 template <int ACT> __device__ __forceinline__ void store_act(void* p, size_t i, float v) {
   if (ACT == SMOE_F32) ((float*)p)[i] = v;
   else ((uint16_t*)p)[i] = (uint16_t)f32_to_bf16_bits(v);
+}
+
+// eight consecutive numbers from a 16-byte aligned place, and back
+template <int ACT> __device__ __forceinline__ void load8(const void* p, size_t i, float (&v)[8]) {
+  if (ACT == SMOE_F32) {
+    const float4 a = *(const float4*)((const float*)p + i), b = *(const float4*)((const float*)p + i + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const uint4 a = *(const uint4*)((const uint16_t*)p + i);
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int j = 0; j < 4; j++) { v[2 * j] = __uint_as_float(u[j] << 16); v[2 * j + 1] = __uint_as_float(u[j] & 0xFFFF0000u); }
+  }
+}
+template <int ACT> __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8]) {
+  if (ACT == SMOE_F32) {
+    *(float4*)((float*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)((float*)p + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) u[j] = pack_bf16_rne(v[2 * j], v[2 * j + 1]);
+    *(uint4*)((uint16_t*)p + i) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
 }
 
 template <int CTRL> __device__ __forceinline__ float dpp_f32(float v) {

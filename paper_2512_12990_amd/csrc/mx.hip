@@ -1,0 +1,235 @@
+// smoe_mx_quantize, smoe_mx_dequantize and smoe_mx_matvec: microscaled 4-bit floats, and the product of a few unquantised
+// rows with them.
+#include "mx.hpp"
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------------------- there and back
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+  return o > v ? o : v;
+}
+
+// A thread takes 8 columns, the four lanes of a quad a block.  The largest magnitude is found on the bit patterns
+// (ordered as the numbers are, NaN last); floor(log2) of it is its exponent field.  Bound: bytes moved.
+template <int SRC>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(const void* src, size_t n8, uint32_t* codes, uint8_t* scales) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;                                        // (whole quads: K is a multiple of 32)
+  float v[8];
+  load8<SRC>(src, i * 8, v);
+  uint32_t big = 0;
+#pragma unroll
+  for (int j = 0; j < 8; j++) { const uint32_t u = __float_as_uint(v[j]) & 0x7FFFFFFFu; big = u > big ? u : big; }
+  big = dpp_max_u32<0xB1>(big);
+  big = dpp_max_u32<0x4E>(big);
+  const uint32_t ex = big >> 23, byte = ex == 255 ? 255u : ex > 2 ? ex - 2 : 0u;
+  const float scale = mx_scale(byte);
+  uint32_t c = 0;
+  if (byte != 255) {                                          // the conversion divides by the scale, rounds to nearest even and saturates at 6
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+  }
+  codes[i] = c;
+  if ((i & 3) == 0) scales[i >> 2] = (uint8_t)byte;
+}
+
+template <int DST>
+__global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t* codes, const uint8_t* scales, size_t n8, void* dst) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  const float scale = mx_scale(scales[i >> 2]);
+  const uint32_t c = codes[i];
+  float v[8];
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
+  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
+  v[0] = a[0] * scale; v[1] = a[1] * scale; v[2] = b[0] * scale; v[3] = b[1] * scale;
+  v[4] = d[0] * scale; v[5] = d[1] * scale; v[6] = e[0] * scale; v[7] = e[1] * scale;
+  store8<DST>(dst, i * 8, v);
+}
+
+static int check_rows(long long rows, int K) {
+  if (rows < 0 || K <= 0 || K % 32 || rows > (1ll << 34) / K) return SMOE_ESHAPE;
+  return SMOE_OK;
+}
+
+extern "C" int smoe_mx_quantize(smoe_ctx* ctx, long long rows, int K, const void* src_dev, int src_dtype, uint8_t* codes_dev, uint8_t* scales_dev) {
+  if (!ctx || (src_dtype != SMOE_F32 && src_dtype != SMOE_BF16)) return SMOE_EINVAL;
+  if (const int rc = check_rows(rows, K)) return rc;
+  if (rows == 0) return SMOE_OK;
+  if (!src_dev || !codes_dev || !scales_dev) return SMOE_EINVAL;
+  if (!aligned16(src_dev) || !aligned16(codes_dev) || !aligned16(scales_dev)) return SMOE_EALIGN;
+  ON_DEVICE_OF(ctx);
+  const size_t n8 = (size_t)rows * K / 8;
+  const unsigned grid = (unsigned)((n8 + 255) / 256);
+  if (src_dtype == SMOE_F32) mx_quantize_kernel<SMOE_F32><<<grid, 256, 0, ctx->stream>>>(src_dev, n8, (uint32_t*)codes_dev, scales_dev);
+  else mx_quantize_kernel<SMOE_BF16><<<grid, 256, 0, ctx->stream>>>(src_dev, n8, (uint32_t*)codes_dev, scales_dev);
+  HIPCHK(ctx, hipGetLastError());
+  return SMOE_OK;
+}
+
+extern "C" int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const uint8_t* codes_dev, const uint8_t* scales_dev, void* dst_dev, int dst_dtype) {
+  if (!ctx || (dst_dtype != SMOE_F32 && dst_dtype != SMOE_BF16)) return SMOE_EINVAL;
+  if (const int rc = check_rows(rows, K)) return rc;
+  if (rows == 0) return SMOE_OK;
+  if (!dst_dev || !codes_dev || !scales_dev) return SMOE_EINVAL;
+  if (!aligned16(dst_dev) || !aligned16(codes_dev) || !aligned16(scales_dev)) return SMOE_EALIGN;
+  ON_DEVICE_OF(ctx);
+  const size_t n8 = (size_t)rows * K / 8;
+  const unsigned grid = (unsigned)((n8 + 255) / 256);
+  if (dst_dtype == SMOE_F32) mx_dequantize_kernel<SMOE_F32><<<grid, 256, 0, ctx->stream>>>((const uint32_t*)codes_dev, scales_dev, n8, dst_dev);
+  else mx_dequantize_kernel<SMOE_BF16><<<grid, 256, 0, ctx->stream>>>((const uint32_t*)codes_dev, scales_dev, n8, dst_dev);
+  HIPCHK(ctx, hipGetLastError());
+  return SMOE_OK;
+}
+
+// ------------------------------------------------------------------------------- a few rows
+// y[slot] = W[idx[slot]] x, W microscaled, x as it is.  Bound: the bytes of the selected matrices.
+//   A work-group takes 16 weight rows of one expert and up to 16 of the slots that chose this expert, so that every weight
+// byte is read once however many tokens share it: the work-group of a slot that is not the first of its expert has
+// nothing to do.  Its four waves share the columns out, 128 at a time; 32 columns of a row are one 16-byte load of a lane.
+//   Codes are expanded to bf16, which holds e2m1 times a power of two exactly, and multiplied by matrix instructions with
+// fp32 sums.  fp32 activations go in as three bf16 numbers whose sum they are (8 + 8 + 8 bits, cut off, not rounded), so
+// these products are exact too.
+struct MatvecArgs {
+  const uint8_t* codes; const uint8_t* scales; const void* x; const int32_t* idx; void* y;
+  int E, N, K, T, k, x_slots, swiglu;
+};
+
+#define MV_WAVES 4
+template <int ACT> __device__ __forceinline__ void store1(void* p, size_t i, float v) {
+  if (ACT == SMOE_F32) ((float*)p)[i] = v;
+  else ((__bf16*)p)[i] = (__bf16)v;
+}
+
+template <int ACT>
+__global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) {
+  constexpr int PARTS = ACT == SMOE_F32 ? 3 : 1;
+  __shared__ int slots[256];
+  __shared__ int wave_n[MV_WAVES + 1];
+  __shared__ float part[MV_WAVES][16][17];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int c = lane & 15, g = lane >> 4;
+  const int n = a.T * a.k, s0 = (int)blockIdx.y;
+  int e = 0, n_mine = n;
+  if (a.idx) {
+    auto expert = [&](int i) { const int v = a.idx[i]; return v < 0 ? 0 : v >= a.E ? a.E - 1 : v; };
+    e = expert(s0);
+    const bool is = tid < n && expert(tid) == e;
+    const uint64_t b = __ballot(is);
+    if (lane == 0) wave_n[wave] = (int)__builtin_popcountll(b);
+    if (tid == 0) wave_n[MV_WAVES] = 0;
+    __syncthreads();
+    int base = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < MV_WAVES; w++) { base += w < wave ? wave_n[w] : 0; total += wave_n[w]; }
+    const int at = base + (int)__builtin_popcountll(b & ((1ull << lane) - 1));
+    if (is) slots[at] = tid;
+    __syncthreads();
+    if (slots[0] != s0) return;                               // (uniform over the work-group)
+    n_mine = total;
+  } else {
+    if (tid < n) slots[tid] = tid;
+    __syncthreads();
+  }
+  const int r0 = (int)blockIdx.x * 16, nb = a.K >> 5;
+  const size_t row = (size_t)e * a.N + r0 + c;
+  const uint8_t* wc = a.codes + row * (size_t)(a.K >> 1);
+  const uint8_t* ws = a.scales + row * (size_t)nb;
+  for (int m0 = 0; m0 < n_mine; m0 += 16) {
+    const int slot = slots[min(m0 + c, n_mine - 1)];
+    const size_t xrow = (size_t)(a.x_slots ? slot : slot / a.k) * a.K;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int u = wave; u * 4 < nb; u += MV_WAVES) {
+      const int blk = u * 4 + g;
+      const bool ok = blk < nb;
+      const int bc = ok ? blk : nb - 1;
+      u32x4 w = *(const u32x4*)(wc + (size_t)bc * 16);
+      const float scale = mx_scale(ws[bc]);
+#pragma unroll
+      for (int s = 0; s < 4; s++) {
+        const uint32_t q = ok ? w[s] : 0u;
+        const float sc = ok ? scale : 1.0f;
+        union { bf16x2 p[4]; bf16x8 v; } wf;
+        wf.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 0);
+        wf.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 1);
+        wf.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 2);
+        wf.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 3);
+        const size_t xi = xrow + (size_t)bc * 32 + s * 8;
+        if constexpr (ACT == SMOE_BF16) {
+          u32x4 xv = *(const u32x4*)((const uint16_t*)a.x + xi);
+          if (!ok) xv = u32x4{0, 0, 0, 0};
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, __builtin_bit_cast(bf16x8, xv), acc, 0, 0, 0);
+        } else {
+          float v[8];
+          load8<SMOE_F32>(a.x, xi, v);
+          union { uint32_t u[4]; bf16x8 v; } p[PARTS];
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            uint32_t h[2][3];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+              float x = ok ? v[2 * i + j] : 0.0f;
+              const bool fin = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+              for (int m = 0; m < 3; m++) {
+                h[j][m] = __float_as_uint(x) & 0xFFFF0000u;
+                if (m == 0 && !fin && (__float_as_uint(x) & 0x7FFFFFu)) h[j][m] |= 0x00400000u;      // NaN stays NaN
+                x = fin ? x - __uint_as_float(h[j][m]) : 0.0f;
+              }
+            }
+#pragma unroll
+            for (int m = 0; m < 3; m++) p[m].u[i] = (h[0][m] >> 16) | h[1][m];
+          }
+#pragma unroll
+          for (int m = PARTS - 1; m >= 0; m--) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, p[m].v, acc, 0, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[wave][4 * g + i][c] = acc[i];
+    __syncthreads();
+    // 256 threads, 16 rows of 16 slots; with SwiGLU the first half, a pair of rows each
+    const int rows = a.swiglu ? 8 : 16, rr = tid % rows, cc = tid / rows;
+    if (cc < 16 && m0 + cc < n_mine) {
+      auto sum = [&](int r) {
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < MV_WAVES; w++) s += part[w][r][cc];
+        return s;
+      };
+      const size_t yrow = (size_t)slots[m0 + cc];
+      if (a.swiglu) {
+        const float gt = sum(2 * rr), up = sum(2 * rr + 1);
+        store1<ACT>(a.y, yrow * (a.N >> 1) + (r0 >> 1) + rr, gt / (1.0f + expf(-gt)) * up);
+      } else {
+        store1<ACT>(a.y, yrow * a.N + r0 + rr, sum(rr));
+      }
+    }
+    __syncthreads();
+  }
+}
+
+extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T, int k,
+                              const void* x_dev, int act_dtype, int x_slots, const int32_t* idx_dev, int swiglu, void* y_dev) {
+  if (!ctx || (act_dtype != SMOE_F32 && act_dtype != SMOE_BF16) || (x_slots != 0 && x_slots != 1) || (swiglu != 0 && swiglu != 1)) return SMOE_EINVAL;
+  if (E <= 0 || E > SMOE_MAX_EXPERTS || T < 0 || T > SMOE_MAX_MULTI || k <= 0 || k > SMOE_MAX_TOPK) return SMOE_ESHAPE;
+  if (const int rc = check_mx_matrix(N, K)) return rc;
+  if (T == 0) return SMOE_OK;
+  if (!idx_dev && (E != 1 || k != 1)) return SMOE_ESHAPE;
+  if (!w_codes_dev || !w_scales_dev || !x_dev || !y_dev || x_dev == y_dev) return SMOE_EINVAL;
+  if (!aligned16(w_codes_dev) || !aligned16(w_scales_dev) || !aligned16(x_dev) || !aligned16(idx_dev) || !aligned16(y_dev)) return SMOE_EALIGN;
+  ON_DEVICE_OF(ctx);
+  const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu};
+  const dim3 grid(N / 16, idx_dev ? T * k : 1);
+  if (act_dtype == SMOE_F32) mx_matvec_kernel<SMOE_F32><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
+  else mx_matvec_kernel<SMOE_BF16><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
+  HIPCHK(ctx, hipGetLastError());
+  return SMOE_OK;
+}

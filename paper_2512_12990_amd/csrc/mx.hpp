@@ -1,0 +1,19 @@
+// Microscaled 4-bit floats: what quantiser and products share.
+//
+// A row of K numbers is K / 2 bytes of codes (two e2m1 codes a byte, the even column in the low nibble) and K / 32 bytes
+// of scales: a block of 32 columns is 16 bytes of codes and one e8m0 byte X + 127, X the block's power of two.  e2m1:
+// sign, then 0 .5 1 1.5 2 3 4 6.  Scale byte 255 makes its block NaN.
+#pragma once
+#include "common.hpp"
+
+// 2^X as a float; X = -127 is a subnormal
+__device__ __forceinline__ float mx_scale(uint32_t byte) {
+  const uint32_t u = byte == 0 ? 0x00400000u : byte == 255 ? 0x7FC00000u : byte << 23;
+  return __uint_as_float(u);
+}
+
+// one expert's matrix [N, K]: byte offsets inside it stay below 2^31
+static inline int check_mx_matrix(int N, int K) {
+  if (N <= 0 || N % 16 || N > (1 << 20) || K <= 0 || K % 32 || K > (1 << 16) || (long long)N * (K / 2) >= (1ll << 31)) return SMOE_ESHAPE;
+  return SMOE_OK;
+}

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) 
       const size_t yrow = (size_t)slots[m0 + cc];
       if (a.swiglu) {
         const float gt = sum(2 * rr), up = sum(2 * rr + 1);
-        store1<ACT>(a.y, yrow * (a.N >> 1) + (r0 >> 1) + rr, gt / (1.0f + expf(-gt)) * up);
+        store1<ACT>(a.y, yrow * (a.N >> 1) + (r0 >> 1) + rr, swiglu(gt, up));
       } else {
         store1<ACT>(a.y, yrow * a.N + r0 + rr, sum(rr));
       }

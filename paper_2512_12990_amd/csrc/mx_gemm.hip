@@ -3,6 +3,8 @@
 //   group    one work-group per expert: the expert's slots, in order, and its tiles of at most BT of them
 //   gemm     a work-group per tile of slots and BN weight rows
 #include "mx.hpp"
+#include <type_traits>
+#include <stdlib.h>
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -19,7 +21,7 @@ struct MxGemmArgs {
   const MxTile* tiles;        // null without rows
   const int* n_tiles;
   void* y;
-  int N, K, n, k, x_slots, col_tiles;
+  int N, K, n, k, x_slots, x_rows, swiglu, out_f32, col_tiles, super;
 };
 
 // Work-group e: slots of expert e to rows[], its tiles to tiles[].  Every work-group counts all slots, so that none waits
@@ -54,85 +56,315 @@ __global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx
   if (e == E - 1 && tid == 0) *n_tiles = tiles_before + nt;
 }
 
-template <int OUT> __device__ __forceinline__ void store1(void* p, size_t i, float v) {
-  if (OUT == SMOE_F32) ((float*)p)[i] = v;
-  else ((__bf16*)p)[i] = (__bf16)v;
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+__device__ __forceinline__ u32x4 buffer_of(const void* base, uint32_t bytes) {
+  const uint64_t v = (uint64_t)base;
+  return u32x4{(uint32_t)uni((int)(uint32_t)v), (uint32_t)uni((int)(uint32_t)(v >> 32)) & 0xFFFFu, (uint32_t)uni((int)bytes), 0x00020000u};
+}
+// 16 or 4 bytes of every lane from memory straight into LDS: lane i's at lds + 16 i or 4 i.  The LDS address is an operand in M0, so the
+// compiler writes that register (one wait state between the write and the load).  It does not count these loads.
+__device__ __forceinline__ void to_lds16(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void to_lds4(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+  asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds) : "memory");
 }
 
-// Four waves side by side over the weight rows; a wave 64 slots by 64 weight rows.
-template <int OUT, int SWIGLU>
-__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs a) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// Shape of a work-group: NT waves along the slots times NN along the weight rows, FT by FN fragments of 32 a wave.
+//   A stage is 256 columns, 128 bytes of codes a row, brought straight into one of NBUF buffers.  The eight 16-byte
+// pieces of a row are stored permuted (piece p at p ^ (row / 2 % 8)), so that sixteen lanes of an operand read, sixteen rows of
+// one piece, fall into different banks.  Half h of a wave multiplies blocks 4h .. 4h + 3 of a stage: its scales of
+// a row are one dword, a byte per step.
+//   Scales come 16 bytes a row at a time, two stages' worth: a dword per stage would cost as many requests to L2 as half the codes (dense product,
+// 4096 slots, N 2048, K 10944: 97 us with, 70 us without such loads).
+template <int NT, int NN, int FT, int FN, int NBUF_> struct MgShape {
+  static constexpr int NW = NT * NN, BT = 32 * NT * FT, BN = 32 * NN * FN, ROWS = BT + BN, NBUF = NBUF_;
+  static constexpr int FRAGS = ROWS / 32, PAIRS = (FRAGS + 1) / 2;
+  static constexpr int LC = ROWS / 8 / NW;                              // code loads of a wave and stage
+  static_assert(ROWS % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && PAIRS <= NW && BN % 64 == 0, "whole loads");
+  static constexpr int codes = ROWS * 128, scales = PAIRS * 1024, extra = PAIRS * 256;      // a code buffer; one of two scale buffers; a fifth dword for each row
+  static constexpr int chunk(bool unal) { return scales + (unal ? extra : 0); }
+  static constexpr int slots_at(bool unal) { return NBUF * codes + 2 * chunk(unal); }       // where the tile's slots stand
+  static constexpr int lds(bool unal) { return slots_at(unal) + BT * 4; }
+  static constexpr int out_row = BN * 4 + 16;                           // epilogue: bytes of a row (fp32 at most; the 16 keep the rows of a fragment in different banks)
+  static_assert(32 * NT * out_row <= NBUF * codes, "a fragment row of the result fits the code buffers");
+};
+
+// UNAL: a row's scales do not begin on a dword (K not a multiple of 128): a fifth dword is fetched, and scales are shifted.
+template <class S, bool UNAL, int NT, int NN, int FT, int FN>
+__device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
+  constexpr int NW = S::NW, BT = S::BT, BN = S::BN, NBUF = S::NBUF, LC = S::LC;
+  constexpr int LCN = BN / 8 / NW, LCT = LC - LCN;                      // code loads of weight rows, of token rows
+  constexpr uint32_t STAGE = S::codes, SCALES = NBUF * STAGE, CHUNK = S::chunk(UNAL);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
-  const int ti = (int)blockIdx.x / a.col_tiles, ct = (int)blockIdx.x % a.col_tiles;
+  // ---- which tile: consecutive items, `super` tiles of slots side by side for every tile of weight rows, stay on one XCD
+  const int n_tiles = a.rows ? uni(*a.n_tiles) : (a.n + BT - 1) / BT;
+  const int n_items = n_tiles * a.col_tiles, run = (n_items + 7) >> 3;
+  const int place = (int)blockIdx.x >> 3, item = ((int)blockIdx.x & 7) * run + place;
+  if (place >= run || item >= n_items) return;
+  const int band = uni(item / (a.super * a.col_tiles)), in_band = item - band * a.super * a.col_tiles;
+  const int band_n = min(a.super, n_tiles - band * a.super);
+  const int ct = uni(in_band / band_n), ti = band * a.super + in_band - ct * band_n;
   MxTile tile;
   if (a.rows) {
-    if (ti >= *a.n_tiles) return;
     tile = a.tiles[ti];
+    tile.expert = uni(tile.expert); tile.first = uni(tile.first); tile.count = uni(tile.count);
   } else {
-    tile = MxTile{0, ti * 64, min(64, a.n - ti * 64), 0};
+    tile = MxTile{0, ti * BT, min(BT, a.n - ti * BT), 0};
   }
-  const int nb = a.K >> 5, n0 = ct * 256 + wave * 64;
-  if (n0 >= a.N) return;
-  const uint8_t *wc[2], *ws[2], *xc[2], *xs[2];
-#pragma unroll
-  for (int f = 0; f < 2; f++) {
-    const size_t wr = (size_t)tile.expert * a.N + min(n0 + f * 32 + c, a.N - 1);
-    const int i = tile.first + min(f * 32 + c, tile.count - 1);
+  const int nb = a.K >> 5, n0 = ct * BN, n_st = (nb + 7) >> 3;
+  const uint32_t rowb = (uint32_t)(a.K >> 1);
+  const u32x4 rwc = buffer_of(a.wc + (size_t)tile.expert * a.N * rowb, (uint32_t)a.N * rowb);
+  const u32x4 rws = buffer_of(a.ws + (size_t)tile.expert * a.N * nb, (uint32_t)a.N * (uint32_t)nb);
+  const u32x4 rxc = buffer_of(a.xc, (uint32_t)a.x_rows * rowb);
+  const u32x4 rxs = buffer_of(a.xs, ((uint32_t)a.x_rows * (uint32_t)nb + 3u) & ~3u);      // (whole dwords: every one fetched holds a byte of the array)
+  auto x_row = [&](int r) {                                            // row of X of the tile's slot r (past the last: the last again)
+    const int i = tile.first + min(r, tile.count - 1);
     const int slot = a.rows ? a.rows[i] : i;
-    const size_t xr = a.x_slots ? slot : slot / a.k;
-    wc[f] = a.wc + wr * (size_t)(a.K >> 1); ws[f] = a.ws + wr * (size_t)nb;
-    xc[f] = a.xc + xr * (size_t)(a.K >> 1); xs[f] = a.xs + xr * (size_t)nb;
+    return (uint32_t)(a.x_slots ? slot : slot / a.k);
+  };
+  int* slots = (int*)(As + S::slots_at(UNAL));                          // for the epilogue
+  if (tid < BT) {
+    const int i = tile.first + min(tid, tile.count - 1);
+    slots[tid] = a.rows ? a.rows[i] : i;
   }
-  f32x16 acc[2][2];
+  // ---- addresses.  Code load q of a wave: rows 8 (NW q + wave) .. + 7 of the stage, weight rows first; a lane's piece is the same for all q
+  constexpr uint32_t NONE = 0x80000000u;                               // beyond every buffer: nothing is fetched
+  const int pr = lane >> 3, piece = (lane & 7) ^ (((8 * wave + pr) >> 1) & 7);
+  const uint32_t wv = (uint32_t)(n0 + 8 * wave + pr) * rowb + piece * 16u;
+  uint32_t xv[LCT > 0 ? LCT : 1];
 #pragma unroll
-  for (int i = 0; i < 2; i++)
+  for (int q = 0; q < LCT; q++) xv[q] = x_row(8 * (NW * q + wave) + pr) * rowb + piece * 16u;
+  const bool piece_last = (n_st - 1) * 8 + piece < nb;                 // the lane's piece exists in the last stage
+  // scale loads: wave w brings fragments 2p and 2p + 1, p = w (or a copy of an earlier pair), a row a lane
+  const int pair = wave % S::PAIRS, sf = 2 * pair + h;
+  const bool of_w = pair < BN / 64;
+  const uint32_t srow = of_w ? (uint32_t)min(n0 + sf * 32 + c, a.N - 1) : x_row(min(sf, S::FRAGS - 1) * 32 - BN + c);
+  const uint32_t sv = srow * (uint32_t)nb;
+  const u32x4 rs = of_w ? rws : rxs;
+  const uint32_t as_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)As;
+  // code loads q0 .. q1 - 1 of the LC that bring stage st into a buffer (past the last stage nothing is fetched, but the load counts)
+  auto issue = [&](int st, uint32_t buf, int q0, int q1) __attribute__((always_inline)) {
+    const uint32_t lds = as_base + buf;
+    const bool skip = st >= n_st || (st == n_st - 1 && !piece_last);
 #pragma unroll
-    for (int j = 0; j < 2; j++)
+    for (int q = q0; q < q1; q++)
+      to_lds16(q < LCN ? rwc : rxc, skip ? NONE : q < LCN ? wv + (uint32_t)(8 * NW * q) * rowb : xv[q < LCN ? 0 : q - LCN], (uint32_t)st * 128u, lds + (NW * q + wave) * 1024u);
+  };
+  constexpr int LSC = UNAL ? 2 : 1;
+  // scales of stages 2g and 2g + 1.  A 16-byte load may run over the row's end (into the next row, or zeros behind the array)
+  auto issue_scales = [&](int g) __attribute__((always_inline)) {
+    const uint32_t lds = as_base + SCALES + (g & 1) * CHUNK + pair * 1024u;
+    const int left = nb - 16 * g;                                      // the row's blocks from this chunk on
+    to_lds16(rs, left <= 0 ? NONE : sv & ~3u, (uint32_t)g * 16u, lds);
+    if (UNAL) to_lds4(rs, left + (int)(sv & 3u) <= 16 ? NONE : (sv & ~3u) + 16u, (uint32_t)g * 16u, as_base + SCALES + (g & 1) * CHUNK + S::scales + pair * 256u);
+  };
+  const int wt = wave % NT, wn = wave / NT;
+  f32x16 acc[FN][FT];
+#pragma unroll
+  for (int i = 0; i < FN; i++)
+#pragma unroll
+    for (int j = 0; j < FT; j++)
 #pragma unroll
       for (int r = 0; r < 16; r++) acc[i][j][r] = 0.0f;
-  for (int b0 = 0; b0 < nb; b0 += 2) {
-    const int b = b0 + h, bc = min(b, nb - 1);
-    i32x8 w[2], x[2];
-    int sw[2], sx[2];
+  // shift of an unaligned row's scales, in bytes
+  uint32_t shw[FN], shx[FT];
 #pragma unroll
-    for (int f = 0; f < 2; f++) {
-      const u32x4 cw = *(const u32x4*)(wc[f] + (size_t)bc * 16), cx = *(const u32x4*)(xc[f] + (size_t)bc * 16);
-      w[f] = i32x8{(int)cw[0], (int)cw[1], (int)cw[2], (int)cw[3], 0, 0, 0, 0};
-      x[f] = i32x8{(int)cx[0], (int)cx[1], (int)cx[2], (int)cx[3], 0, 0, 0, 0};
-      // past the last block: both scales 2^-127, the products vanish
-      sw[f] = b < nb ? ws[f][bc] : 0;
-      sx[f] = b < nb ? xs[f][bc] : 0;
-    }
+  for (int i = 0; i < FN; i++) shw[i] = UNAL ? ((uint32_t)min(n0 + (wn * FN + i) * 32 + c, a.N - 1) * (uint32_t)nb) & 3u : 0u;
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+  for (int j = 0; j < FT; j++) shx[j] = UNAL ? (x_row((wt * FT + j) * 32 + c) * (uint32_t)nb) & 3u : 0u;
+  // scales of fragment f, dword 2 (st % 2) + hh of the row's four
+  auto scale_of = [&](int st, int f, int hh, uint32_t sh) __attribute__((always_inline)) {
+    const uint8_t* at = As + SCALES + ((st >> 1) & 1) * CHUNK;
+    const int d = 2 * (st & 1) + hh;
+    const uint32_t o = f * 512 + c * 16 + d * 4;
+    const uint32_t lo = *(const uint32_t*)(at + o);
+    if (!UNAL) return lo;
+    const uint32_t hi = *(const uint32_t*)(at + (d == 3 ? (uint32_t)(S::scales + f * 128 + c * 4) : o + 4));
+    return (uint32_t)__builtin_amdgcn_alignbyte(hi, lo, sh);
+  };
+  const uint32_t swz = (uint32_t)((c >> 1) & 7);
+  struct Frags { u32x4 w[FN], x[FT]; };
+  auto read = [&](const uint8_t* st, int p, Frags& f) __attribute__((always_inline)) {
+    const uint32_t o = c * 128 + (((uint32_t)p ^ swz) * 16);
 #pragma unroll
-      for (int j = 0; j < 2; j++) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[i], x[j], acc[i][j], 4, 4, 0, sw[i], 0, sx[j]);
+    for (int i = 0; i < FN; i++) f.w[i] = *(const u32x4*)(st + (wn * FN + i) * 4096 + o);
+#pragma unroll
+    for (int j = 0; j < FT; j++) f.x[j] = *(const u32x4*)(st + (BN / 32 + wt * FT + j) * 4096 + o);
+  };
+  auto wide = [](u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+  // one step: FN FT products of 64 columns; `extra(m)` follows product m
+  auto mul = [&](auto s_c, const Frags& f, const uint32_t (&sw)[FN], const uint32_t (&sx)[FT], auto extra) __attribute__((always_inline)) {
+    constexpr int s = decltype(s_c)::value;
+#pragma unroll
+    for (int i = 0; i < FN; i++)
+#pragma unroll
+      for (int j = 0; j < FT; j++) {
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(f.w[i]), wide(f.x[j]), acc[i][j], 4, 4, s, (int)sw[i], s, (int)sx[j]);
+        extra(i * FT + j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  const std::integral_constant<int, 0> s0{};
+  const std::integral_constant<int, 1> s1{};
+  const std::integral_constant<int, 2> s2{};
+  const std::integral_constant<int, 3> s3{};
+  auto read_scales = [&](int st, uint32_t (&sw)[FN], uint32_t (&sx)[FT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FN; i++) sw[i] = scale_of(st, wn * FN + i, h, shw[i]);
+#pragma unroll
+    for (int j = 0; j < FT; j++) sx[j] = scale_of(st, BN / 32 + wt * FT + j, h, shx[j]);
+  };
+  // ---- columns.  The operands of a step are read while the one before it is multiplied; in front of a stage's last step comes the
+  // barrier behind which the stage has been read by all and the next one is there.  The LC loads into the buffer so freed are dealt to the
+  // products of the following steps: a direct load keeps the texture path busy for some 22 cycles, and eight waves that send
+  // all theirs at once stand still meanwhile.  With two buffers the loads go to three of the four steps, so that the last of them has a step's time.
+  constexpr int QS = NBUF == 2 ? 3 : 4;
+  constexpr int HEAD = LC / QS;                                        // loads dealt to the step behind the barrier
+  constexpr int M = FN * FT;
+  auto deal = [&](int st, uint32_t buf, int quarter, int m) __attribute__((always_inline)) {
+    if (quarter >= QS) return;
+    const int q0 = LC * quarter / QS, n = LC * (quarter + 1) / QS - q0;
+    issue(st, buf, q0 + n * m / M, q0 + n * (m + 1) / M);
+  };
+  const int n_full = nb >> 3;
+  issue_scales(0);
+  issue_scales(1);
+#pragma unroll
+  for (int st = 0; st < NBUF - 1; st++) issue(st, st * STAGE, 0, LC);
+  issue(NBUF - 1, (NBUF - 1) * STAGE, 0, HEAD);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC + HEAD) : "memory");
+  uint32_t cur = 0, before = (NBUF - 1) * STAGE;                       // buffer of the stage, and of the one before it
+  uint32_t sw[FN], sx[FT];
+  Frags f0, f1;
+  if (n_full > 0) {
+    read_scales(0, sw, sx);
+    read(As, 4 * h, f0);
   }
-  // lane: slot c of the fragment, weight rows 8 (r / 4) + 4 h + r % 4
+  for (int st = 0; st < n_full; st++) {
+    const uint8_t* at = As + cur;
+    const uint32_t next = cur == (NBUF - 1) * STAGE ? 0 : cur + STAGE;
+    const int ahead = st + NBUF - 1;
+    read(at, 4 * h + 1, f1);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(s0, f0, sw, sx, [&](int m) __attribute__((always_inline)) { deal(ahead, before, 1, m); });
+    read(at, 4 * h + 2, f0);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(s1, f1, sw, sx, [&](int m) __attribute__((always_inline)) { deal(ahead, before, 2, m); });
+    read(at, 4 * h + 3, f1);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(s2, f0, sw, sx, [&](int m) __attribute__((always_inline)) { deal(ahead, before, 3, m); });
+    // younger than stage st + 1: NBUF - 2 stages of codes, and with three buffers the scales sent for behind an odd stage
+    if (NBUF > 2 && (st & 1) == 0 && st > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC + LSC) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC) : "memory");
+    uint32_t nw[FN], nx[FT];
+    read_scales(st + 1, nw, nx);
+    read(As + next, 4 * h, f0);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(s3, f1, sw, sx, [&](int m) __attribute__((always_inline)) { deal(st + NBUF, cur, 0, m); });
+    if (st & 1) issue_scales(((st + 1) >> 1) + 1);
 #pragma unroll
-  for (int j = 0; j < 2; j++) {
-    if (j * 32 + c >= tile.count) continue;
-    const int at = tile.first + j * 32 + c;
-    const size_t slot = a.rows ? a.rows[at] : at;
+    for (int i = 0; i < FN; i++) sw[i] = nw[i];
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int j = 0; j < FT; j++) sx[j] = nx[j];
+    before = cur;
+    cur = next;
+  }
+  if (n_full < n_st) {
+    // the last blocks: half h takes `half` of them from h * half on; one that does not exist gets the scale 2^-127 on both sides,
+    // and its products vanish (whatever codes LDS holds there)
+    const uint8_t* at = As + cur;
+    const int left = nb - n_full * 8, half = (left + 1) >> 1, mine = min(half, left - h * half);
+    const uint32_t mask = mine >= 4 ? 0xFFFFFFFFu : (1u << (8 * max(mine, 0))) - 1u;
+    auto pick = [&](int f, uint32_t sh) __attribute__((always_inline)) {
+      const uint64_t v = ((uint64_t)scale_of(n_full, f, 1, sh) << 32) | scale_of(n_full, f, 0, sh);
+      return (uint32_t)(v >> (8 * h * half)) & mask;
+    };
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const int nr = n0 + i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-        if (nr >= a.N) continue;
-        const float v0 = acc[i][j][r], v1 = acc[i][j][r + 1];
-        if (SWIGLU) {
-          store1<OUT>(a.y, slot * (size_t)(a.N >> 1) + (nr >> 1), v0 / (1.0f + expf(-v0)) * v1);
+    for (int i = 0; i < FN; i++) sw[i] = pick(wn * FN + i, shw[i]);
+#pragma unroll
+    for (int j = 0; j < FT; j++) sx[j] = pick(BN / 32 + wt * FT + j, shx[j]);
+    for (int s = 0; s < half; s++) {
+      Frags f;
+      read(at, h * half + s, f);
+      mul(s0, f, sw, sx, [](int) {});
+#pragma unroll
+      for (int i = 0; i < FN; i++) sw[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < FT; j++) sx[j] >>= 8;
+    }
+  }
+  // ---- result.  Lane: slot c of a fragment, weight rows 8 (r / 4) + 4 h + r % 4.  A row of fragments at a time goes through LDS, so that
+  // whole lines of Y are written (stores of 4 or 8 bytes straight from the lanes: 22 of 96 us, 2048 tokens, top-4 of 60, N 2816, K 2048).
+  const int osz = a.out_f32 ? 4 : 2, sg = a.swiglu;
+  const int row_n = (sg ? BN >> 1 : BN), n_out = sg ? a.N >> 1 : a.N, c0 = sg ? n0 >> 1 : n0;      // columns of the tile's rows, of Y, the tile's first
+  const int lpr = 31 - __builtin_clz((unsigned)(row_n * osz / 16));                                // log2 of a row's 16-byte pieces
+#pragma unroll
+  for (int j = 0; j < FT; j++) {
+    // (the first time: no load is on its way to LDS any more, and every wave has read its operands)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(0) : "memory");
+    if (FT > 1 && j * 32 >= tile.count) break;                          // (no wave has slots in these rows)
+    uint8_t* o = As + (wt * 32 + c) * S::out_row;
+#pragma unroll
+    for (int i = 0; i < FN; i++)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int nr = (wn * FN + i) * 32 + 2 * r + 4 * h;
+        const float v0 = acc[i][j][r], v1 = acc[i][j][r + 1], v2 = acc[i][j][r + 2], v3 = acc[i][j][r + 3];
+        if (sg) {
+          const float o0 = swiglu(v0, v1), o1 = swiglu(v2, v3);
+          if (a.out_f32) *(float2*)(o + (nr >> 1) * 4) = make_float2(o0, o1);
+          else *(uint32_t*)(o + (nr >> 1) * 2) = pack_bf16_rne(o0, o1);
         } else {
-          store1<OUT>(a.y, slot * (size_t)a.N + nr, v0);
-          store1<OUT>(a.y, slot * (size_t)a.N + nr + 1, v1);
+          if (a.out_f32) *(float4*)(o + nr * 4) = make_float4(v0, v1, v2, v3);
+          else *(uint2*)(o + nr * 2) = make_uint2(pack_bf16_rne(v0, v1), pack_bf16_rne(v2, v3));
         }
       }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int x = tid; x < (32 * NT) << lpr; x += 64 * NW) {
+      const int lr = x >> lpr, p = x & ((1 << lpr) - 1);
+      const int tr = ((lr >> 5) * FT + j) * 32 + (lr & 31), col = c0 + p * (16 / osz);
+      if (tr < tile.count && col < n_out)                              // (N is a multiple of 16: sixteen bytes are in or out)
+        *(uint4*)((uint8_t*)a.y + ((size_t)slots[tr] * n_out + col) * osz) = *(const uint4*)(As + lr * S::out_row + p * 16);
+    }
   }
+}
+
+template <bool UNAL, int NT, int NN, int FT, int FN, int NBUF>
+__global__ __launch_bounds__(64 * NT * NN) void mx_gemm_kernel(MxGemmArgs a) {
+  extern __shared__ __align__(1024) uint8_t mdyn[];
+  mx_gemm_tile<MgShape<NT, NN, FT, FN, NBUF>, UNAL, NT, NN, FT, FN>(a, mdyn);
 }
 
 static inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct MxShape { int bt, bn; };
+static const MxShape g_shapes[5] = {{32, 128}, {64, 128}, {128, 128}, {128, 256}, {256, 256}};
+static int pick_shape(int n, int E, int N) {
+  if (const char* f = getenv("MXS")) return atoi(f);
+  const int per = n / E;
+  return per <= 24 ? 0 : per <= 48 ? 1 : per <= 96 ? 2 : 4;
+}
+
+template <bool UNAL, int NT, int NN, int FT, int FN, int NBUF>
+static int launch_gemm_t(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int slot) {
+  const size_t lds = MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL);
+  static_assert(MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL) <= 160 * 1024, "LDS");
+  size_t& granted = ctx->mx_lds_granted[slot * 2 + UNAL];
+  if (lds > 64u * 1024u && granted < lds) {      // once per context: beyond the default 64 KB
+    HIPCHK(ctx, hipFuncSetAttribute((const void*)mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    granted = lds;
+  }
+  mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF><<<grid, 64 * NT * NN, lds, ctx->stream>>>(a);
+  HIPCHK(ctx, hipGetLastError());
+  return SMOE_OK;
+}
+template <int NT, int NN, int FT, int FN, int NBUF>
+static int launch_gemm(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int slot) {
+  return (a.K >> 5) % 4 ? launch_gemm_t<true, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot) : launch_gemm_t<false, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot);
+}
 
 struct MxProductLayout { size_t rows, tiles, n_tiles, total; };
 static MxProductLayout product_layout(int T, int k, int E) {
@@ -172,10 +404,15 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
   const MxProductLayout l = product_layout(T, k, E);
   if (idx_dev && scratch_bytes < l.total) return SMOE_ESIZE;
   ON_DEVICE_OF(ctx);
-  const int n = T * k, bt = 64;
+  const int n = T * k;
   uint8_t* s = (uint8_t*)scratch_dev;
-  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, y_dev, N, K, n, k, x_slots, (N + 255) / 256};
+  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, y_dev, N, K, n, k, x_slots, T * (x_slots ? k : 1), swiglu,
+               out_dtype == SMOE_F32, 0, 1};
+  const int shape = pick_shape(n, E, N);
+  const int bt = g_shapes[shape].bt;
+  a.col_tiles = (N + g_shapes[shape].bn - 1) / g_shapes[shape].bn;
   int max_tiles = (n + bt - 1) / bt;
+  a.super = max_tiles / E < 1 ? 1 : max_tiles / E > 8 ? 8 : max_tiles / E;
   if (idx_dev) {
     int32_t* rows = (int32_t*)(s + l.rows);
     MxTile* tiles = (MxTile*)(s + l.tiles);
@@ -185,14 +422,12 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
     a.rows = rows; a.tiles = tiles; a.n_tiles = n_tiles;
     max_tiles = n / bt + (n < E ? n : E);
   }
-  const unsigned grid = (unsigned)max_tiles * (unsigned)a.col_tiles;
-  if (out_dtype == SMOE_F32) {
-    if (swiglu) mx_gemm_kernel<SMOE_F32, 1><<<grid, 256, 0, ctx->stream>>>(a);
-    else mx_gemm_kernel<SMOE_F32, 0><<<grid, 256, 0, ctx->stream>>>(a);
-  } else {
-    if (swiglu) mx_gemm_kernel<SMOE_BF16, 1><<<grid, 256, 0, ctx->stream>>>(a);
-    else mx_gemm_kernel<SMOE_BF16, 0><<<grid, 256, 0, ctx->stream>>>(a);
+  const unsigned grid = ((unsigned)max_tiles * (unsigned)a.col_tiles + 7) / 8 * 8;
+  switch (shape) {
+    case 0: return launch_gemm<1, 4, 1, 1, 3>(ctx, a, grid, 0);
+    case 1: return launch_gemm<2, 2, 1, 2, 3>(ctx, a, grid, 1);
+    case 2: return launch_gemm<2, 2, 2, 2, 2>(ctx, a, grid, 2);
+    case 3: return launch_gemm<2, 4, 2, 2, 3>(ctx, a, grid, 3);
+    default: return launch_gemm<2, 4, 4, 2, 2>(ctx, a, grid, 4);
   }
-  HIPCHK(ctx, hipGetLastError());
-  return SMOE_OK;
 }

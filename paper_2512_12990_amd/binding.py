@@ -7,6 +7,7 @@ if the library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -126,6 +127,7 @@ class Ctx:
         self.device = device
         s = stream if stream is not None else torch.cuda.current_stream(device)
         self._stream = s
+        self.raw_stream, self.torch_device = s.cuda_stream, torch.device("cuda", device)
         self.workspace, base = None, 0
         if workspace_bytes:                       # 0: a context for the calls that need no workspace
             self.workspace = torch.empty(workspace_bytes + 256, dtype=torch.uint8, device="cuda:%d" % device)
@@ -344,6 +346,13 @@ SCORES = {"softmax": 0, "sigmoid": 1}
 GROUP_SCORES = {"max": 0, "top2": 1}
 
 
+_ACTS = {torch.float32, torch.bfloat16}
+_F32, _BF16, _I32, _U8 = {torch.float32}, {torch.bfloat16}, {torch.int32}, {torch.uint8}
+_ONE = {torch.float32: _F32, torch.bfloat16: _BF16}
+_stream_now = torch._C._cuda_getCurrentRawStream
+_empty = torch.empty
+
+
 def _arg(ok: bool, what: str):
     if not ok:
         raise SmoeError("invalid argument: " + what)
@@ -351,102 +360,109 @@ def _arg(ok: bool, what: str):
 
 def _t(ctx: Ctx, name: str, t: torch.Tensor, dtypes, shape=None) -> int:
     """Address of a tensor after the checks that the C entry cannot make."""
+    if t.dtype in dtypes and (shape is None or t.shape == shape) and t.get_device() == ctx.device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype not in dtypes:
         raise SmoeError("%s: dtype %s" % (name, t.dtype))
     if shape is not None and t.shape != shape:
         raise SmoeError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if t.device.type != "cuda" or t.device.index != ctx.device or not t.is_contiguous():
-        raise SmoeError("%s: must be contiguous on device %d of the context" % (name, ctx.device))
-    return t.data_ptr()
+    raise SmoeError("%s: must be contiguous on device %d of the context" % (name, ctx.device))
 
 
-_ACTS = (torch.float32, torch.bfloat16)
-_F32, _I32, _U8 = (torch.float32,), (torch.int32,), (torch.uint8,)
+def _tensors(values):
+    for v in values:
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, tuple):
+            yield from _tensors(v)
 
 
-class _OnStream:
-    """Makes the context's stream torch's current one, so that what is allocated inside belongs to it; tensors of another stream
-    that the call uses are kept from reuse until its work on the context's stream is done, and what it made (`keep`) until the
-    caller's work on its own stream is."""
-
-    def __init__(self, ctx: Ctx, *tensors):
-        self.s = self.caller = None
-        now = torch._C._cuda_getCurrentRawStream(ctx.device)
-        if now != ctx._stream.cuda_stream:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(ctx._stream)
-            self.caller = torch.cuda.current_stream(ctx.device)
-            self.s = torch.cuda.stream(ctx._stream)
-
-    def __enter__(self):
-        if self.s is not None:
-            self.s.__enter__()
-        return self
-
-    def keep(self, *made):
-        if self.caller is not None:
-            for t in made:
-                if t is not None:
-                    t.record_stream(self.caller)
-
-    def __exit__(self, *a):
-        if self.s is not None:
-            self.s.__exit__(*a)
+def _on_stream(f):
+    """Runs a call with the context's stream as torch's current one, so that what it allocates belongs to that stream.  Where the caller's is another,
+    the tensors that the call uses are kept from reuse until its work on the context's stream is done, and what it returns until
+    the caller's work on its own stream is; the order of the two streams' work is the caller's."""
+    @functools.wraps(f)
+    def call(ctx, *args, **kw):
+        if _stream_now(ctx.device) == ctx.raw_stream:
+            return f(ctx, *args, **kw)
+        caller = torch.cuda.current_stream(ctx.device)
+        for t in _tensors((args, tuple(kw.values()))):
+            if t.is_cuda:
+                t.record_stream(ctx._stream)
+        with torch.cuda.stream(ctx._stream):
+            out = f(ctx, *args, **kw)
+        for t in _tensors((out,)):
+            t.record_stream(caller)
+        return out
+    return call
 
 
+@_on_stream
 def smoe_route_scores(ctx: Ctx, k: int, logits: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None,
                       w_router: Optional[torch.Tensor] = None, score: str = "softmax", n_group: int = 1, topk_group: int = 1,
                       group_score: str = "max", bias: Optional[torch.Tensor] = None, norm_topk: bool = False, routed_scale: float = 1.0):
     """(idx int32 [T, k], w float32 [T, k]); logits float32 [T, E], or x [T, d] and w_router float32 [E, d]."""
-    _arg(score in SCORES, "score %r" % (score,))
-    _arg(group_score in GROUP_SCORES, "group_score %r" % (group_score,))
+    if score not in SCORES or group_score not in GROUP_SCORES:
+        raise SmoeError("invalid argument: score %r, group_score %r" % (score, group_score))
     if logits is not None:
         _arg(logits.dim() == 2, "logits [T, E]")
-        (T, E), d, act = logits.shape, 0, F32
-        lp, xp, wp = _t(ctx, "logits", logits, _F32), None, None
+        T, E = logits.shape
+        d, act, lp, xp, wp = 0, F32, _t(ctx, "logits", logits, _F32), None, None
     else:
         _arg(x is not None and w_router is not None and x.dim() == 2 and w_router.dim() == 2, "logits, or x [T, d] and w_router [E, d]")
         (T, d), E = x.shape, w_router.shape[0]
         lp, xp, wp = None, _t(ctx, "x", x, _ACTS), _t(ctx, "w_router", w_router, _F32, (E, d))
         act = _DT[x.dtype]
     bp = None if bias is None else _t(ctx, "bias", bias, _F32, (E,))
-    with _OnStream(ctx, logits, x, w_router, bias) as on:
-        idx = torch.empty((T, k), dtype=torch.int32, device="cuda:%d" % ctx.device)
-        w = torch.empty((T, k), dtype=torch.float32, device="cuda:%d" % ctx.device)
-        _chk(lib().smoe_route_scores(ctx.h, T, E, k, d, lp, xp, act, wp, SCORES[score], n_group, topk_group, GROUP_SCORES[group_score], bp,
-                                     int(norm_topk), routed_scale, idx.data_ptr(), w.data_ptr()), "smoe_route_scores", ctx.h)
-        on.keep(idx, w)
+    _arg(k > 0, "k")
+    like = x if logits is None else logits
+    idx, w = like.new_empty((T, k), dtype=torch.int32), like.new_empty((T, k), dtype=torch.float32)
+    rc = lib().smoe_route_scores(ctx.h, T, E, k, d, lp, xp, act, wp, SCORES[score], n_group, topk_group, GROUP_SCORES[group_score], bp,
+                                 norm_topk, routed_scale, idx.data_ptr(), w.data_ptr())
+    if rc:
+        _chk(rc, "smoe_route_scores", ctx.h)
     return idx, w
 
 
+@_on_stream
 def smoe_residual_norm(ctx: Ctx, res: Optional[torch.Tensor], y: Optional[torch.Tensor] = None, slot_w: Optional[torch.Tensor] = None,
                        post_w: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0,
                        pre_w: Optional[torch.Tensor] = None, eps: float = 1e-6, res_out: Optional[torch.Tensor] = None, want_x: bool = True,
                        act_dtype: Optional[torch.dtype] = None):
     """(res_out [T, d], x [T, d] or None).  y [T, k, d] or [T, d]; without y the act dtype is pre_w's or `act_dtype`; without
     res the residual has the act dtype.  res_out may be res (in place)."""
-    first = y if y is not None else res
-    _arg(first is not None and first.dim() in (2, 3) and first.dim() == (2 if y is None else y.dim()), "y [T, k, d] or [T, d], res [T, d]")
-    T, d = first.shape[0], first.shape[-1]
-    k = 0 if y is None else y.shape[1] if y.dim() == 3 else 1
-    act = y.dtype if y is not None else act_dtype or (pre_w.dtype if pre_w is not None else res.dtype)
-    _arg(act in _ACTS and (act_dtype is None or act_dtype == act), "act dtype")
-    acts = (act,)
+    if y is not None:
+        ys = y.shape
+        _arg(len(ys) in (2, 3), "y [T, k, d] or [T, d]")
+        T, d, k, act = ys[0], ys[-1], ys[1] if len(ys) == 3 else 1, y.dtype
+    else:
+        _arg(res is not None and res.dim() == 2, "y, or res [T, d]")
+        T, d = res.shape
+        k, act = 0, act_dtype or (pre_w.dtype if pre_w is not None else res.dtype)
+    if act not in _ACTS or (act_dtype is not None and act_dtype != act):
+        raise SmoeError("invalid argument: act dtype %s" % act)
+    acts = _ONE[act]
     yp = None if y is None else _t(ctx, "y", y, acts)
     rp = None if res is None else _t(ctx, "res", res, _ACTS, (T, d))
     sp = None if slot_w is None else _t(ctx, "slot_w", slot_w, _F32, (T, k))
     op = None if post_w is None else _t(ctx, "post_w", post_w, acts, (d,))
     pp = None if pre_w is None else _t(ctx, "pre_w", pre_w, acts, (d,))
-    gp = None if gate is None else _t(ctx, "gate", gate, acts, (d,) if gate.dim() == 1 else (T, d))
-    with _OnStream(ctx, res, y, slot_w, post_w, gate, pre_w, res_out) as on:
-        if res_out is None:
-            res_out = torch.empty((T, d), dtype=act if res is None else res.dtype, device="cuda:%d" % ctx.device)
-        x = torch.empty((T, d), dtype=act, device="cuda:%d" % ctx.device) if want_x else None
-        ro = _t(ctx, "res_out", res_out, _ACTS if res is None else (res.dtype,), (T, d))
-        _chk(lib().smoe_residual_norm(ctx.h, T, d, k, yp, sp, op, gp, int(gate is not None and gate.dim() == 2), scale, rp, pp, eps, _DT[act],
-                                      _DT[res_out.dtype], ro, x.data_ptr() if want_x else None), "smoe_residual_norm", ctx.h)
-        on.keep(res_out, x)
+    gr = gate is not None and gate.dim() == 2
+    gp = None if gate is None else _t(ctx, "gate", gate, acts, (T, d) if gr else (d,))
+    rd = act if res is None else res.dtype
+    if res_out is None:
+        res_out = _empty((T, d), dtype=rd, device=ctx.torch_device) if res is None else torch.empty_like(res)
+        ro = res_out.data_ptr()
+    else:
+        rd = res_out.dtype if res is None else rd
+        ro = _t(ctx, "res_out", res_out, _ACTS if res is None else _ONE[rd], (T, d))
+    x, xo = None, None
+    if want_x:
+        x = torch.empty_like(res_out) if rd == act else res_out.new_empty((T, d), dtype=act)
+        xo = x.data_ptr()
+    rc = lib().smoe_residual_norm(ctx.h, T, d, k, yp, sp, op, gp, gr, scale, rp, pp, eps, _DT[act], _DT[rd], ro, xo)
+    if rc:
+        _chk(rc, "smoe_residual_norm", ctx.h)
     return res_out, x
 
 
@@ -457,99 +473,112 @@ class Mx(NamedTuple):
 
 
 def _mx(ctx: Ctx, name: str, m: Mx):
+    """(codes address, scales address, shape of the codes)"""
     c, s = m
     cp, sp = _t(ctx, name + ".codes", c, _U8), _t(ctx, name + ".scales", s, _U8)
-    if c.dim() < 2 or c.shape[:-1] != s.shape[:-1] or c.shape[-1] != 16 * s.shape[-1]:
-        raise SmoeError("%s: codes %s and scales %s do not belong together" % (name, tuple(c.shape), tuple(s.shape)))
-    return cp, sp
+    cs, ss = c.shape, s.shape
+    if len(cs) < 2 or cs[:-1] != ss[:-1] or cs[-1] != 16 * ss[-1] or not cs[-1]:
+        raise SmoeError("%s: codes %s and scales %s do not belong together" % (name, tuple(cs), tuple(ss)))
+    return cp, sp, cs
 
 
+@_on_stream
 def smoe_mx_quantize(ctx: Ctx, src: torch.Tensor, out: Optional[Mx] = None) -> Mx:
     """src [..., K] float32 or bfloat16, at least two-dimensional."""
     _arg(src.dim() >= 2 and src.shape[-1] % 32 == 0 and src.shape[-1] > 0, "src [..., K], K a multiple of 32")
-    sp, K = _t(ctx, "src", src, _ACTS), src.shape[-1]
-    with _OnStream(ctx, src, *(out or ())) as on:
-        if out is None:
-            dev = "cuda:%d" % ctx.device
-            out = Mx(torch.empty(src.shape[:-1] + (K // 2,), dtype=torch.uint8, device=dev),
-                     torch.empty(src.shape[:-1] + (K // 32,), dtype=torch.uint8, device=dev))
-            cp, ep = out.codes.data_ptr(), out.scales.data_ptr()
-        else:
-            cp, ep = _mx(ctx, "out", out)
-            _arg(out[0].shape == src.shape[:-1] + (K // 2,), "out: shape")
-        _chk(lib().smoe_mx_quantize(ctx.h, src.numel() // K, K, sp, _DT[src.dtype], cp, ep), "smoe_mx_quantize", ctx.h)
-        on.keep(*out)
+    *lead, K = src.shape
+    sp = _t(ctx, "src", src, _ACTS)
+    if out is None:
+        out = Mx(src.new_empty((*lead, K // 2), dtype=torch.uint8), src.new_empty((*lead, K // 32), dtype=torch.uint8))
+        cp, ep = out[0].data_ptr(), out[1].data_ptr()
+    else:
+        cp, ep, shape = _mx(ctx, "out", out)
+        _arg(shape == (*lead, K // 2), "out: shape")
+    rc = lib().smoe_mx_quantize(ctx.h, src.numel() // K, K, sp, _DT[src.dtype], cp, ep)
+    if rc:
+        _chk(rc, "smoe_mx_quantize", ctx.h)
     return out
 
 
+@_on_stream
 def smoe_mx_dequantize(ctx: Ctx, m: Mx, dtype: torch.dtype = torch.float32) -> torch.Tensor:
-    cp, sp = _mx(ctx, "m", m)
+    cp, sp, (*lead, half) = _mx(ctx, "m", m)
     _arg(dtype in _ACTS, "dtype")
-    K = 2 * m[0].shape[-1]
-    with _OnStream(ctx, *m) as on:
-        out = torch.empty(m[0].shape[:-1] + (K,), dtype=dtype, device="cuda:%d" % ctx.device)
-        _chk(lib().smoe_mx_dequantize(ctx.h, out.numel() // K if K else 0, K, cp, sp, out.data_ptr(), _DT[dtype]), "smoe_mx_dequantize", ctx.h)
-        on.keep(out)
+    out = m[0].new_empty((*lead, 2 * half), dtype=dtype)
+    rc = lib().smoe_mx_dequantize(ctx.h, out.numel() // (2 * half), 2 * half, cp, sp, out.data_ptr(), _DT[dtype])
+    if rc:
+        _chk(rc, "smoe_mx_dequantize", ctx.h)
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def smoe_mx_product_bytes(T: int, k: int, E: int) -> int:
     n = C.c_size_t()
     _chk(lib().smoe_mx_product_bytes(T, k, E, C.byref(n)), "smoe_mx_product_bytes")
     return n.value
 
 
-def _mx_args(ctx: Ctx, w: Mx, x_shape, K: int, idx: Optional[torch.Tensor], swiglu: bool):
-    """(codes, scales, E, N, T, k, x_slots, idx address, shape of y) of a product; x [T, K] or [T, k, K], w [E, N, K] or [N, K]."""
-    wc, ws = _mx(ctx, "w", w)
-    shape = w[0].shape
-    _arg(len(shape) in (2, 3) and 2 * shape[-1] == K, "w [E, N, K] or [N, K] with the K of x")
+def _mx_args(ctx: Ctx, w: Mx, x_shape, idx: Optional[torch.Tensor]):
+    """(codes, scales, E, N, T, k, x_slots, idx address) of a product; x_shape [T, K / 2] or [T, k, K / 2], w [E, N, K] or [N, K]."""
+    wc, ws, shape = _mx(ctx, "w", w)
+    nx = len(x_shape)
+    if len(shape) not in (2, 3) or nx not in (2, 3) or shape[-1] != x_shape[-1]:
+        raise SmoeError("invalid argument: w [E, N, K] or [N, K], x [T, K] or [T, k, K]")
     E, N = (1, shape[0]) if len(shape) == 2 else shape[:2]
-    _arg(len(x_shape) in (2, 3), "x [T, K] or [T, k, K]")
     T = x_shape[0]
     if idx is None:
-        _arg(len(x_shape) == 2 or x_shape[1] == 1, "x [T, K] without idx")
-        k, ip = 1, None
-    else:
-        _arg(idx.dim() == 2, "idx [T, k]")
-        k = idx.shape[1]
-        ip = _t(ctx, "idx", idx, _I32, (T, k))
-        _arg(len(x_shape) == 2 or x_shape[1] == k, "x [T, k, K] with the k of idx")
-    return wc, ws, E, N, T, k, int(len(x_shape) == 3), ip, (T, k, N // 2 if swiglu else N)
+        _arg(nx == 2 or x_shape[1] == 1, "x [T, K] without idx")
+        return wc, ws, E, N, T, 1, nx == 3, None
+    _arg(idx.dim() == 2, "idx [T, k]")
+    k = idx.shape[1]
+    _arg(nx == 2 or x_shape[1] == k, "x [T, k, K] with the k of idx")
+    return wc, ws, E, N, T, k, nx == 3, _t(ctx, "idx", idx, _I32, (T, k))
 
 
+@_on_stream
 def smoe_mx_product(ctx: Ctx, w: Mx, x: Mx, idx: Optional[torch.Tensor] = None, swiglu: bool = False, out_dtype: torch.dtype = torch.bfloat16,
                     scratch: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [T, k, N] (N / 2 with swiglu); w [E, N, K] or [N, K], x [T, K] or [T, k, K], idx int32 [T, k] or None (one matrix, k = 1)."""
-    xc, xs = _mx(ctx, "x", x)
-    K = 2 * x[0].shape[-1]
-    wc, ws, E, N, T, k, slots, ip, shape = _mx_args(ctx, w, x[0].shape, K, idx, swiglu)
-    _arg(out_dtype in _ACTS, "out_dtype")
-    with _OnStream(ctx, *w, *x, idx, scratch, y) as on:
-        need = smoe_mx_product_bytes(T, k, E) if idx is not None else 0
-        if scratch is None and need:
-            scratch = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % ctx.device)
-        if y is None:
-            y = torch.empty(shape, dtype=out_dtype, device="cuda:%d" % ctx.device)
-        _chk(lib().smoe_mx_product(ctx.h, E, N, K, wc, ws, T, k, xc, xs, slots, ip, int(swiglu), _DT[out_dtype],
-                                   None if scratch is None else _t(ctx, "scratch", scratch, _U8), 0 if scratch is None else scratch.numel(),
-                                   _t(ctx, "y", y, (out_dtype,), shape)), "smoe_mx_product", ctx.h)
-        on.keep(y)
+    xc, xs, x_shape = _mx(ctx, "x", x)
+    wc, ws, E, N, T, k, slots, ip = _mx_args(ctx, w, x_shape, idx)
+    if out_dtype not in _ACTS:
+        raise SmoeError("invalid argument: out_dtype %s" % out_dtype)
+    shape = (T, k, N // 2 if swiglu else N)
+    sp, size = None, 0
+    if scratch is not None:
+        sp, size = _t(ctx, "scratch", scratch, _U8), scratch.numel()
+    elif ip is not None and T:
+        size = smoe_mx_product_bytes(T, k, E)
+        scratch = x[0].new_empty(size)
+        sp = scratch.data_ptr()
+    if y is None:
+        y = x[0].new_empty(shape, dtype=out_dtype)
+        yp = y.data_ptr()
+    else:
+        yp = _t(ctx, "y", y, _ONE[out_dtype], shape)
+    rc = lib().smoe_mx_product(ctx.h, E, N, 2 * x_shape[-1], wc, ws, T, k, xc, xs, slots, ip, swiglu, _DT[out_dtype], sp, size, yp)
+    if rc:
+        _chk(rc, "smoe_mx_product", ctx.h)
     return y
 
 
+@_on_stream
 def smoe_mx_matvec(ctx: Ctx, w: Mx, x: torch.Tensor, idx: Optional[torch.Tensor] = None, swiglu: bool = False,
                    y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [T, k, N] (N / 2 with swiglu) of x's dtype, T <= 16; w, idx as in smoe_mx_product, x [T, K] or [T, k, K]."""
     xp = _t(ctx, "x", x, _ACTS)
-    _arg(x.dim() in (2, 3), "x [T, K] or [T, k, K]")
-    wc, ws, E, N, T, k, slots, ip, shape = _mx_args(ctx, w, x.shape, x.shape[-1], idx, swiglu)
-    with _OnStream(ctx, *w, x, idx, y) as on:
-        if y is None:
-            y = torch.empty(shape, dtype=x.dtype, device="cuda:%d" % ctx.device)
-        _chk(lib().smoe_mx_matvec(ctx.h, E, N, x.shape[-1], wc, ws, T, k, xp, _DT[x.dtype], slots, ip, int(swiglu),
-                                  _t(ctx, "y", y, (x.dtype,), shape)), "smoe_mx_matvec", ctx.h)
-        on.keep(y)
+    xs = x.shape
+    _arg(len(xs) > 1, "x [T, K] or [T, k, K]")
+    wc, ws, E, N, T, k, slots, ip = _mx_args(ctx, w, xs[:-1] + (xs[-1] // 2,), idx)
+    shape = (T, k, N // 2 if swiglu else N)
+    if y is None:
+        y = x.new_empty(shape)
+        yp = y.data_ptr()
+    else:
+        yp = _t(ctx, "y", y, _ONE[x.dtype], shape)
+    rc = lib().smoe_mx_matvec(ctx.h, E, N, xs[-1], wc, ws, T, k, xp, _DT[x.dtype], slots, ip, swiglu, yp)
+    if rc:
+        _chk(rc, "smoe_mx_matvec", ctx.h)
     return y
 
 

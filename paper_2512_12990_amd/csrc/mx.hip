@@ -91,15 +91,16 @@ extern "C" int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const ui
 
 // ------------------------------------------------------------------------------- a few rows
 // y[slot] = W[idx[slot]] x, W microscaled, x as it is.  Bound: the bytes of the selected matrices.
-//   A work-group takes 16 weight rows of one expert and up to 16 of the slots that chose this expert, so that every weight
-// byte is read once however many tokens share it: the work-group of a slot that is not the first of its expert has
-// nothing to do.  Its four waves share the columns out, 128 at a time; 32 columns of a row are one 16-byte load of a lane.
+//   A work-group takes 16 RT weight rows of one expert and up to 16 of the slots that chose this expert, so that every weight
+// byte is read once however many tokens share it.  Work-groups go by slots (that of a slot that is not the first of its expert has
+// nothing to do) or, with fewer experts than slots, by experts.  Its four waves share the columns out, 128 at a time (32 columns of a row are one 16-byte load of a lane), and add their
+// sums up through LDS.
 //   Codes are expanded to bf16, which holds e2m1 times a power of two exactly, and multiplied by matrix instructions with
 // fp32 sums.  fp32 activations go in as three bf16 numbers whose sum they are (8 + 8 + 8 bits, cut off, not rounded), so
-// these products are exact too.
+// these products are exact too; the splitting is seven vector instructions a number, which is why it serves RT tiles of rows at once.
 struct MatvecArgs {
   const uint8_t* codes; const uint8_t* scales; const void* x; const int32_t* idx; void* y;
-  int E, N, K, T, k, x_slots, swiglu;
+  int E, N, K, T, k, x_slots, swiglu, by_expert;
 };
 
 #define MV_WAVES 4
@@ -108,112 +109,153 @@ template <int ACT> __device__ __forceinline__ void store1(void* p, size_t i, flo
   else ((__bf16*)p)[i] = (__bf16)v;
 }
 
-template <int ACT>
+// eight activations as they lie in memory, and as PARTS operands of a matrix instruction
+template <int ACT> struct RawX { u32x4 v[ACT == SMOE_F32 ? 2 : 1]; };
+template <int ACT, int PARTS>
+__device__ __forceinline__ void operands(const RawX<ACT>& r, bool ok, bf16x8 (&p)[PARTS]) {
+  if constexpr (ACT == SMOE_BF16) {
+    p[0] = __builtin_bit_cast(bf16x8, ok ? r.v[0] : u32x4{0, 0, 0, 0});
+  } else {
+    union { uint32_t u[4]; bf16x8 v; } o[3];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      uint32_t h[2][3];
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        const uint32_t u = ok ? r.v[i >> 1][2 * (i & 1) + j] : 0u;
+        const float x = __uint_as_float(u);
+        h[j][0] = u & 0xFFFF0000u;
+        // (an infinity leaves nothing; a NaN whose bits were cut off leaves a NaN)
+        const float rest = (u & 0x7FFFFFFFu) == 0x7F800000u ? 0.0f : x - __uint_as_float(h[j][0]);
+        h[j][1] = __float_as_uint(rest) & 0xFFFF0000u;
+        h[j][2] = __float_as_uint(rest - __uint_as_float(h[j][1]));
+      }
+#pragma unroll
+      for (int m = 0; m < 3; m++) o[m].u[i] = __builtin_amdgcn_perm(h[1][m], h[0][m], 0x07060302u);
+    }
+#pragma unroll
+    for (int m = 0; m < 3; m++) p[m] = o[m].v;
+  }
+}
+
+template <int ACT, int RT, int U>      // U: units of 128 columns in flight
 __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) {
-  constexpr int PARTS = ACT == SMOE_F32 ? 3 : 1;
-  __shared__ int slots[256];
-  __shared__ int wave_n[MV_WAVES + 1];
-  __shared__ float part[MV_WAVES][16][17];
+  constexpr int PARTS = ACT == SMOE_F32 ? 3 : 1, ROWS = 16 * RT;
+  __shared__ int slots[SMOE_MAX_MULTI * SMOE_MAX_TOPK];
+  __shared__ int wave_n[MV_WAVES];
+  __shared__ float part[MV_WAVES][ROWS][17];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c = lane & 15, g = lane >> 4;
   const int n = a.T * a.k, s0 = (int)blockIdx.y;
   int e = 0, n_mine = n;
-  if (a.idx) {
-    auto expert = [&](int i) { const int v = a.idx[i]; return v < 0 ? 0 : v >= a.E ? a.E - 1 : v; };
-    e = expert(s0);
+  auto expert = [&](int i) { const int v = a.idx[i]; return v < 0 ? 0 : v >= a.E ? a.E - 1 : v; };
+  if (a.T == 1) {                                             // every slot by itself
+    if (a.idx) e = expert(s0);
+    n_mine = 1;
+  } else if (a.idx) {
+    e = a.by_expert ? s0 : expert(s0);
     const bool is = tid < n && expert(tid) == e;
     const uint64_t b = __ballot(is);
     if (lane == 0) wave_n[wave] = (int)__builtin_popcountll(b);
-    if (tid == 0) wave_n[MV_WAVES] = 0;
     __syncthreads();
     int base = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < MV_WAVES; w++) { base += w < wave ? wave_n[w] : 0; total += wave_n[w]; }
-    const int at = base + (int)__builtin_popcountll(b & ((1ull << lane) - 1));
-    if (is) slots[at] = tid;
+    if (is) slots[base + (int)__builtin_popcountll(b & ((1ull << lane) - 1))] = tid;
     __syncthreads();
-    if (slots[0] != s0) return;                               // (uniform over the work-group)
+    if (total == 0 || (!a.by_expert && slots[0] != s0)) return;      // (uniform over the work-group)
     n_mine = total;
   } else {
     if (tid < n) slots[tid] = tid;
     __syncthreads();
   }
-  const int r0 = (int)blockIdx.x * 16, nb = a.K >> 5;
-  const size_t row = (size_t)e * a.N + r0 + c;
-  const uint8_t* wc = a.codes + row * (size_t)(a.K >> 1);
-  const uint8_t* ws = a.scales + row * (size_t)nb;
+  const int r0 = (int)blockIdx.x * ROWS, nb = a.K >> 5;
+  const uint8_t* wc[RT];
+  const uint8_t* ws[RT];
+#pragma unroll
+  for (int t = 0; t < RT; t++) {
+    const size_t row = (size_t)e * a.N + min(r0 + 16 * t + c, a.N - 1);
+    wc[t] = a.codes + row * (size_t)(a.K >> 1);
+    ws[t] = a.scales + row * (size_t)nb;
+  }
+  const int units = (nb + 3) >> 2, per = (units + MV_WAVES - 1) / MV_WAVES, u_end = min(units, (wave + 1) * per);
   for (int m0 = 0; m0 < n_mine; m0 += 16) {
-    const int slot = slots[min(m0 + c, n_mine - 1)];
+    const int slot = a.T == 1 ? s0 : slots[min(m0 + c, n_mine - 1)];
     const size_t xrow = (size_t)(a.x_slots ? slot : slot / a.k) * a.K;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int u = wave; u * 4 < nb; u += MV_WAVES) {
-      const int blk = u * 4 + g;
-      const bool ok = blk < nb;
-      const int bc = ok ? blk : nb - 1;
-      u32x4 w = *(const u32x4*)(wc + (size_t)bc * 16);
-      const float scale = mx_scale(ws[bc]);
+    f32x4 acc[RT];
 #pragma unroll
-      for (int s = 0; s < 4; s++) {
-        const uint32_t q = ok ? w[s] : 0u;
-        const float sc = ok ? scale : 1.0f;
-        union { bf16x2 p[4]; bf16x8 v; } wf;
-        wf.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 0);
-        wf.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 1);
-        wf.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 2);
-        wf.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc, 3);
-        const size_t xi = xrow + (size_t)bc * 32 + s * 8;
-        if constexpr (ACT == SMOE_BF16) {
-          u32x4 xv = *(const u32x4*)((const uint16_t*)a.x + xi);
-          if (!ok) xv = u32x4{0, 0, 0, 0};
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, __builtin_bit_cast(bf16x8, xv), acc, 0, 0, 0);
-        } else {
-          float v[8];
-          load8<SMOE_F32>(a.x, xi, v);
-          union { uint32_t u[4]; bf16x8 v; } p[PARTS];
+    for (int t = 0; t < RT; t++) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int u0 = wave * per; u0 < u_end; u0 += U) {
+      u32x4 w[U][RT];
+      uint32_t sb[U][RT];
+      RawX<ACT> x[U][4];
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            uint32_t h[2][3];
+      for (int u = 0; u < U; u++) {
+        const int bc = min((u0 + u) * 4 + g, nb - 1);
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-              float x = ok ? v[2 * i + j] : 0.0f;
-              const bool fin = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+        for (int t = 0; t < RT; t++) {
+          w[u][t] = *(const u32x4*)(wc[t] + (size_t)bc * 16);
+          sb[u][t] = ws[t][bc];
+        }
 #pragma unroll
-              for (int m = 0; m < 3; m++) {
-                h[j][m] = __float_as_uint(x) & 0xFFFF0000u;
-                if (m == 0 && !fin && (__float_as_uint(x) & 0x7FFFFFu)) h[j][m] |= 0x00400000u;      // NaN stays NaN
-                x = fin ? x - __uint_as_float(h[j][m]) : 0.0f;
-              }
-            }
+        for (int s = 0; s < 4; s++)
 #pragma unroll
-            for (int m = 0; m < 3; m++) p[m].u[i] = (h[0][m] >> 16) | h[1][m];
+          for (int v = 0; v < (ACT == SMOE_F32 ? 2 : 1); v++)
+            x[u][s].v[v] = *(const u32x4*)((const uint8_t*)a.x + (xrow + (size_t)bc * 32 + s * 8) * (ACT == SMOE_F32 ? 4 : 2) + v * 16);
+      }
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        // a block that does not exist: activations and codes 0
+        const bool ok = u0 + u < u_end && (u0 + u) * 4 + g < nb;
+        float sc[RT];
+#pragma unroll
+        for (int t = 0; t < RT; t++) sc[t] = ok ? mx_scale(sb[u][t]) : 1.0f;
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+          bf16x8 p[PARTS];
+          operands<ACT>(x[u][s], ok, p);
+#pragma unroll
+          for (int t = 0; t < RT; t++) {
+            const uint32_t q = w[u][t][s];
+            union { bf16x2 h[4]; bf16x8 v; } wf;
+            wf.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 0);
+            wf.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 1);
+            wf.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 2);
+            wf.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 3);
+#pragma unroll
+            for (int m = PARTS - 1; m >= 0; m--) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, p[m], acc[t], 0, 0, 0);
           }
-#pragma unroll
-          for (int m = PARTS - 1; m >= 0; m--) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, p[m].v, acc, 0, 0, 0);
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; i++) part[wave][4 * g + i][c] = acc[i];
+    for (int t = 0; t < RT; t++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) part[wave][16 * t + 4 * g + i][c] = acc[t][i];
     __syncthreads();
-    // 256 threads, 16 rows of 16 slots; with SwiGLU the first half, a pair of rows each
-    const int rows = a.swiglu ? 8 : 16, rr = tid % rows, cc = tid / rows;
-    if (cc < 16 && m0 + cc < n_mine) {
+    const int rows = a.swiglu ? ROWS / 2 : ROWS, cols = min(16, n_mine - m0);
+    for (int i = tid; i < rows * cols; i += 64 * MV_WAVES) {
+      const int rr = i % rows, cc = i / rows;
       auto sum = [&](int r) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < MV_WAVES; w++) s += part[w][r][cc];
         return s;
       };
-      const size_t yrow = (size_t)slots[m0 + cc];
+      const size_t yrow = (size_t)(a.T == 1 ? s0 : slots[m0 + cc]);
       if (a.swiglu) {
-        const float gt = sum(2 * rr), up = sum(2 * rr + 1);
-        store1<ACT>(a.y, yrow * (a.N >> 1) + (r0 >> 1) + rr, swiglu(gt, up));
+        if (r0 + 2 * rr < a.N) store1<ACT>(a.y, yrow * (a.N >> 1) + (r0 >> 1) + rr, swiglu(sum(2 * rr), sum(2 * rr + 1)));
       } else {
-        store1<ACT>(a.y, yrow * a.N + r0 + rr, sum(rr));
+        if (r0 + rr < a.N) store1<ACT>(a.y, yrow * a.N + r0 + rr, sum(rr));
       }
     }
     __syncthreads();
   }
+}
+
+template <int ACT, int RT, int U> static void launch_matvec(smoe_ctx* ctx, const MatvecArgs& a) {
+  const dim3 grid((a.N + 16 * RT - 1) / (16 * RT), !a.idx ? 1 : a.by_expert ? a.E : a.T * a.k);
+  mx_matvec_kernel<ACT, RT, U><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
 }
 
 extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T, int k,
@@ -226,10 +268,20 @@ extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t*
   if (!w_codes_dev || !w_scales_dev || !x_dev || !y_dev || x_dev == y_dev) return SMOE_EINVAL;
   if (!aligned16(w_codes_dev) || !aligned16(w_scales_dev) || !aligned16(x_dev) || !aligned16(idx_dev) || !aligned16(y_dev)) return SMOE_EALIGN;
   ON_DEVICE_OF(ctx);
-  const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu};
-  const dim3 grid(N / 16, idx_dev ? T * k : 1);
-  if (act_dtype == SMOE_F32) mx_matvec_kernel<SMOE_F32><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
-  else mx_matvec_kernel<SMOE_BF16><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
+  const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu, T > 1 && E < T * k};
+  // Rows of a work-group.  Four tiles share one fetch and one splitting of the activations, with one unit of columns in flight, so that many work-groups fit
+  // a CU; where that leaves too few work-groups, one tile and two units.  16 tokens, top-6 of 64, N 2048, K 1408, fp32: 32 us with four tiles, 73 with one;
+  // one token, N 8192, K 8192, bf16: 19.4 us with four (128 work-groups), 13.3 with one; one token, top-6, N 2816, K 2048, bf16 (264): 11.6 and 10.2; four
+  // tokens, top-4 of 60, the same matrices (704): 17.3 and 17.7; fp32, one token, top-6, N 2048, K 1408 (192): 8.2 and 10.8; 16 tokens,
+  // N 21888, K 2048, bf16 (342): 14.8 and 19.2.
+  const long long wgs = (long long)((N + 63) / 64) * (!idx_dev ? 1 : T * k < E ? T * k : E);
+  if (act_dtype == SMOE_F32) {
+    if (wgs < 128) launch_matvec<SMOE_F32, 1, 2>(ctx, a);
+    else launch_matvec<SMOE_F32, 4, 1>(ctx, a);
+  } else {
+    if (wgs < (T > 4 ? 256 : 512)) launch_matvec<SMOE_BF16, 1, 2>(ctx, a);
+    else launch_matvec<SMOE_BF16, 4, 1>(ctx, a);
+  }
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;
 }

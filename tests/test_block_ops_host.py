@@ -176,7 +176,7 @@ def test_mx_matvec_refuses(ctx, kw, rc):
 
 
 class _FakeCtx:
-    device, h = 0, None
+    device, h, raw_stream = 0, None, 0
 
 
 @pytest.mark.parametrize("call", [
@@ -190,11 +190,15 @@ class _FakeCtx:
     lambda c: B.smoe_residual_norm(c, torch.zeros(4, 64, dtype=torch.float16)),
     lambda c: B.smoe_residual_norm(c, torch.zeros(4, 64), act_dtype=torch.float16),
     lambda c: B.smoe_mx_quantize(c, torch.zeros(32)),
+    lambda c: B.smoe_mx_quantize(c, torch.zeros(())),
+    lambda c: B.smoe_mx_quantize(c, torch.zeros(4, 0)),
     lambda c: B.smoe_mx_quantize(c, torch.zeros(4, 48)),
     lambda c: B.smoe_mx_quantize(c, torch.zeros(4, 64, dtype=torch.float16)),
     lambda c: B.smoe_mx_dequantize(c, B.Mx(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8))),
     lambda c: B.smoe_mx_matvec(c, B.Mx(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8)), torch.zeros(4, 64)),
+    lambda c: B.smoe_mx_matvec(c, B.Mx(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8)), torch.zeros(())),
 ])
-def test_binding_refuses(call):
+def test_binding_refuses(call, monkeypatch):
+    monkeypatch.setattr(B, "_stream_now", lambda device: 0)              # (no device to ask here)
     with pytest.raises(B.SmoeError):
         call(_FakeCtx())

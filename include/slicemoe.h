@@ -169,7 +169,7 @@ int smoe_route(smoe_ctx* ctx, int T, int E, int k, int d_model, const float* log
  * largest where the group has one expert), and the topk_group best groups stay.  idx_dev[t,0..k) = the k largest c_e in
  * them from the highest down; equal scores go to the lower group and the lower expert.  w_dev[t,j] = s of the chosen
  * expert, divided by the sum of the chosen ones if norm_topk, times routed_scale.  Scores, sums and comparisons are
- * binary64, weights are rounded to fp32 once.
+ * binary64 (two numbers nearer than 2^-51 may compare either way), weights are rounded to fp32 once.
  *   A logit of minus infinity scores 0 (a masked expert: chosen only where nothing else is left); a token without any
  * other logit gets weights 0.  A NaN ranks below every number: with softmax it makes the token's weights NaN, with sigmoid
  * the expert's own (and with norm_topk those beside it).

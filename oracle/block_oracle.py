@@ -49,22 +49,29 @@ def product(w, x, idx, swiglu):
 
 
 # ----------------------------------------------------------------------------------------- routing
+def scores(z, score):
+    z = z.astype(np.float64)
+    if score == "sigmoid":
+        with np.errstate(over="ignore"):
+            return 1.0 / (1.0 + np.exp(-z))
+    out = np.empty_like(z)
+    for t in range(z.shape[0]):
+        real = z[t][~np.isnan(z[t])]
+        m = real.max() if len(real) else -np.inf
+        with np.errstate(invalid="ignore"):
+            p = np.where(z[t] == -np.inf, 0.0, np.where(z[t] == m, 1.0, np.exp(z[t] - m)))
+        out[t] = p if p.sum() == 0 else p / p.sum()
+    return out
+
+
 def route_scores(z, k, score, n_group, topk_group, group_score, bias, norm, scale):
     T, E = z.shape
-    z = z.astype(np.float64)
+    all_scores = scores(z, score)
     bias = np.zeros(E) if bias is None else bias.astype(np.float64)
     idx, w = np.empty((T, k), np.int64), np.empty((T, k))
     size = E // n_group
     for t in range(T):
-        if score == "sigmoid":
-            with np.errstate(over="ignore"):
-                s = 1.0 / (1.0 + np.exp(-z[t]))
-        else:
-            real = z[t][~np.isnan(z[t])]
-            m = real.max() if len(real) else -np.inf
-            with np.errstate(invalid="ignore"):
-                p = np.where(z[t] == -np.inf, 0.0, np.where(z[t] == m, 1.0, np.exp(z[t] - m)))
-            s = p if p.sum() == 0 else p / p.sum()
+        s = all_scores[t]
         c = s + bias
         rank = lambda v: -np.inf if np.isnan(v) else v
         # a NaN comes after minus infinity

@@ -137,70 +137,83 @@ __device__ __forceinline__ void select_scores_wave(const ScoreArgs& a, int t, co
   }
 }
 
-// ---- short form, E = 64 NJ at most and groups that are whole lanes: lane l holds the NJ experts from NJ l on, everything is ordered by fp32 keys, and a
+// ---- short form: sixteen lanes per token, lane r of them with the NJ experts from NJ r on, ordered by fp32 keys.  A
 // token whose keys lie too close together to be sure of the binary64 order is left to select_scores_wave.
 //   The key of an expert is its logit where the order of the scores is the logits' own (no bias; no sum of two scores), else the fp32 score
 // plus bias.  A score is off by at most 5 half steps of 1 (of a sigmoid: argument of the exponential s (1 - s) |z| 1.5 < 0.4, exponential 0.5, sum 1, reciprocal 2;
 // of a softmax: argument 1, exponential 2, divisor and product 2) and the sum with a bias below 4 by one of its own: two keys more than
 // 2^-20 max(1, |key|) apart are in order.  Logits more than 2^-30 apart, and where they decide
 // sigmoids at most 15, have binary64 scores that differ (slope of the sigmoid at 15: 3e-7).
-__device__ __forceinline__ float wave_fmax(float v) { return unorderable(wave_umax(orderable(v))); }
-
+//   Bound: vector issue, about 90 instructions a pick for the four tokens of a wave.  16384 tokens, 256 experts in 8 groups, top-8: 39 us with the long form alone,
+// 28 us with a short form of one token per wave.
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+// the four steps of a reduction over a row of sixteen lanes: neighbour, neighbouring pair, other four of eight, other eight
+#define ROW_REDUCE(v, OP)      \
+  v = OP(v, dpp_u32<0xB1>(v)); \
+  v = OP(v, dpp_u32<0x4E>(v)); \
+  v = OP(v, dpp_u32<0x141>(v)); \
+  v = OP(v, dpp_u32<0x140>(v));
+__device__ __forceinline__ uint32_t row_umax(uint32_t v) { ROW_REDUCE(v, max) return v; }
+__device__ __forceinline__ uint32_t row_umin(uint32_t v) { ROW_REDUCE(v, min) return v; }
+__device__ __forceinline__ float row_fmax(float v) { return unorderable(row_umax(orderable(v))); }
+__device__ __forceinline__ double row_sum64(double v) {
+  v += dpp_f64<0xB1>(v);
+  v += dpp_f64<0x4E>(v);
+  v += dpp_f64<0x141>(v);
+  v += dpp_f64<0x140>(v);
+  return v;
+}
 template <int CTRL> __device__ __forceinline__ void merge_top2(float& b0, float& b1) {
   const float o0 = dpp_f32<CTRL>(b0), o1 = dpp_f32<CTRL>(b1);
   b1 = fmaxf(fminf(b0, o0), fmaxf(b1, o1));
   b0 = fmaxf(b0, o0);
 }
 
-// false: nothing is written, the token needs the long form
+// Token t by sixteen lanes (rl: the lane's number among them).  False in all of them: nothing was written, the token needs the long form.
 template <int NJ>
-__device__ __forceinline__ bool select_scores_short(const ScoreArgs& a, int t, const float* z, int lane) {
-  const int E = a.r.E, k = a.r.k;
-  const bool in = lane * NJ < E, sigmoid = a.score == SMOE_SCORE_SIGMOID;
-  float zv[NJ], v[NJ];
-  if (NJ == 4) {
-    const float4 q = in ? *(const float4*)(z + lane * 4) : make_float4(0, 0, 0, 0);
-    zv[0] = q.x; zv[NJ > 1 ? 1 : 0] = q.y; zv[NJ > 2 ? 2 : 0] = q.z; zv[NJ > 3 ? 3 : 0] = q.w;
-  } else if (NJ == 2) {
-    const float2 q = in ? *(const float2*)(z + lane * 2) : make_float2(0, 0);
-    zv[0] = q.x; zv[NJ > 1 ? 1 : 0] = q.y;
-  } else {
-    zv[0] = in ? z[lane] : 0.0f;
-  }
-  bool fine = true;
+__device__ __forceinline__ bool select_scores_row(const ScoreArgs& a, int t, bool write, int lane) {
+  const int E = a.r.E, k = a.r.k, rl = lane & 15;
+  const bool in = rl * NJ < E, sigmoid = a.score == SMOE_SCORE_SIGMOID;      // (E is a multiple of 4: experts of the last lane may be missing, by fours)
+  const float* z = a.r.logits + (size_t)t * E;
+  float zv[NJ], v[NJ], bias[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; j++) fine = fine && (fabsf(zv[j]) < 80.0f || zv[j] == -INFINITY);
-  float bias[NJ];
+  for (int j = 0; j < NJ; j += 4) {
+    const bool have = rl * NJ + j < E;
+    const float4 q = have ? *(const float4*)(z + rl * NJ + j) : make_float4(0, 0, 0, 0);
+    const float4 b = have && a.r.bias ? *(const float4*)(a.r.bias + rl * NJ + j) : make_float4(0, 0, 0, 0);
+    zv[j] = q.x; zv[j + 1] = q.y; zv[j + 2] = q.z; zv[j + 3] = q.w;
+    bias[j] = b.x; bias[j + 1] = b.y; bias[j + 2] = b.z; bias[j + 3] = b.w;
+  }
+  uint32_t zbig = 0, bbig = 0;                                          // largest magnitudes, as bit patterns (NaN above all)
 #pragma unroll
   for (int j = 0; j < NJ; j++) {
-    bias[j] = a.r.bias && in ? a.r.bias[lane * NJ + j] : 0.0f;
-    fine = fine && fabsf(bias[j]) < 4.0f;
+    const uint32_t u = __float_as_uint(zv[j]);
+    zbig = max(zbig, u == 0xFF800000u ? 0u : u & 0x7FFFFFFFu);
+    bbig = max(bbig, __float_as_uint(bias[j]) & 0x7FFFFFFFu);
   }
-  if (__ballot(!fine)) return false;                                    // (NaN, plus infinity, a bias as a mask)
+  bool fine = zbig < __float_as_uint(80.0f) && bbig < __float_as_uint(4.0f);      // not: NaN, plus infinity, a bias as a mask
   const bool by_score = a.r.bias || (a.n_group > 1 && a.group_score == SMOE_GROUP_TOP2);
   const bool need_den = !sigmoid && (by_score || !a.r.norm_topk);
   float m = 0.0f;
   double den = 1.0;
   if (!sigmoid) {
-    float top = zv[0];
+    float top = -INFINITY;
 #pragma unroll
-    for (int j = 1; j < NJ; j++) top = fmaxf(top, zv[j]);
-    m = wave_fmax(in ? top : -INFINITY);
-    if (m == -INFINITY) return false;
-  }
-  if (need_den) {
-    den = 0.0;
+    for (int j = 0; j < NJ; j++) top = fmaxf(top, rl * NJ + j < E ? zv[j] : -INFINITY);
+    m = row_fmax(top);
+    fine = fine && m > -INFINITY;
+    if (need_den) {
+      den = 0.0;
 #pragma unroll
-    for (int j = 0; j < NJ; j++) den += in ? exp((double)zv[j] - (double)m) : 0.0;
-    den = wave_sum64(den);
+      for (int j = 0; j < NJ; j++) den += rl * NJ + j < E ? exp((double)zv[j] - (double)m) : 0.0;
+      den = row_sum64(den);
+    }
   }
   if (by_score) {
     const float r_den = (float)(1.0 / den);
 #pragma unroll
-    for (int j = 0; j < NJ; j++) {
-      v[j] = sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(zv[j] * -1.44269502f)) : __builtin_amdgcn_exp2f((zv[j] - m) * 1.44269502f) * r_den;
-      v[j] += bias[j];
-    }
+    for (int j = 0; j < NJ; j++)
+      v[j] = (sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(zv[j] * -1.44269502f)) : __builtin_amdgcn_exp2f((zv[j] - m) * 1.44269502f) * r_den) + bias[j];
   } else {
 #pragma unroll
     for (int j = 0; j < NJ; j++) v[j] = zv[j];
@@ -209,85 +222,90 @@ __device__ __forceinline__ bool select_scores_short(const ScoreArgs& a, int t, c
   auto apart = [&](float hi, float lo) { return hi - lo > unit * (by_score ? fmaxf(1.0f, fabsf(hi)) : 1.0f); };
   uint32_t ord[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; j++) ord[j] = in ? orderable(v[j]) : 0u;
+  for (int j = 0; j < NJ; j++) ord[j] = rl * NJ + j < E ? orderable(v[j]) : 0u;
   if (a.n_group > 1) {
-    const int lpg = a.group_size / NJ;                                  // lanes of a group: a power of two
+    const int lpg = a.group_size / NJ;                                  // lanes of a group: a power of two up to 8
     float b0 = v[0], b1 = -INFINITY;
 #pragma unroll
     for (int j = 1; j < NJ; j++) { b1 = fmaxf(b1, fminf(b0, v[j])); b0 = fmaxf(b0, v[j]); }
     if (lpg > 1) merge_top2<0xB1>(b0, b1);
     if (lpg > 2) merge_top2<0x4E>(b0, b1);
-    if (lpg > 4) merge_top2<0x141>(b0, b1);                             // row_half_mirror: the other four of eight
-    if (lpg > 8) merge_top2<0x140>(b0, b1);                             // row_mirror: the other eight of sixteen
-    if (lpg > 16) {
-      const float o0 = __shfl_xor(b0, 16), o1 = __shfl_xor(b1, 16);
-      b1 = fmaxf(fminf(b0, o0), fmaxf(b1, o1)); b0 = fmaxf(b0, o0);
-    }
-    const bool two = a.group_score == SMOE_GROUP_TOP2 && a.group_size > 1;
+    if (lpg > 4) merge_top2<0x141>(b0, b1);
+    const bool two = a.group_score == SMOE_GROUP_TOP2;
     const float score = two ? b0 + b1 : b0;
     int rank = 0;
-    const int mine = lane / lpg;
+    const int mine = rl / lpg;
     for (int g = 0; g < a.n_group; g++) {
-      const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(score), g * lpg));
+      const float o = __shfl(score, (lane & 48) + g * lpg);
       rank += o > score || (o == score && g < mine);
     }
     const bool chosen = rank < a.topk_group;
     if (a.topk_group < a.n_group) {
-      const float worst = -wave_fmax(in && chosen ? -score : -INFINITY), best_out = wave_fmax(in && !chosen ? score : -INFINITY);
+      const float worst = -row_fmax(in && chosen ? -score : -INFINITY), best_out = row_fmax(in && !chosen ? score : -INFINITY);
       // (two sums of two, each number off by up to 9 half steps of 1, each sum by 10 of its own; equal logits without a bias are equal scores)
-      if (!apart(worst, best_out + (two ? 4.0f * unit : 0.0f)) && (by_score || worst != best_out)) return false;
-      if (!by_score && sigmoid && worst > 15.0f) return false;
+      fine = fine && (apart(worst, best_out + (two ? 4.0f * unit : 0.0f)) || (!by_score && worst == best_out));
+      fine = fine && (by_score || !sigmoid || worst <= 15.0f);
     }
-    if (!chosen)
 #pragma unroll
-      for (int j = 0; j < NJ; j++) ord[j] = 0u;
+    for (int j = 0; j < NJ; j++) ord[j] = chosen ? ord[j] : 0u;
   }
   // k picks and, where there is one, the best that is left
   int mysel = 0;
-  float myz = 0.0f, last = 0.0f;
+  float last = 0.0f;
   const int avail = a.topk_group * a.group_size;
   for (int r = 0; r <= k && r < avail; r++) {
-    uint32_t best = ord[0];
-    int jb = 0;
-    float zb = zv[0];
+    uint32_t top = ord[0];
 #pragma unroll
-    for (int j = 1; j < NJ; j++) if (ord[j] > best) { best = ord[j]; jb = j; zb = zv[j]; }
-    const uint32_t top = wave_umax(best);
+    for (int j = 1; j < NJ; j++) top = max(top, ord[j]);
+    top = row_umax(top);
     const float vt = unorderable(top);
-    if (r > 0 && !apart(last, vt) && (by_score || last != vt)) return false;
-    if (!by_score && sigmoid && vt > 15.0f) return false;
+    fine = fine && (r == 0 || apart(last, vt) || (!by_score && last == vt)) && (by_score || !sigmoid || vt <= 15.0f);
     last = vt;
-    const int ls = (int)__builtin_ctzll(__ballot(best == top));         // the lowest index among equal keys
     if (r == k) break;
-    const int js = __builtin_amdgcn_readlane(jb, ls);
-    const float zs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(zb), ls));
-    if (lane == r) { mysel = ls * NJ + js; myz = zs; }
+    uint32_t mine = 0xFFFFu;                                            // the lowest index among equal keys
 #pragma unroll
-    for (int j = 0; j < NJ; j++) if (lane == ls && jb == j) ord[j] = 0u;
+    for (int j = NJ - 1; j >= 0; j--) mine = ord[j] == top ? (uint32_t)(rl * NJ + j) : mine;
+    const uint32_t e = row_umin(mine);
+    if (rl == r) mysel = (int)e;
+    const int at = (int)e - rl * NJ;
+#pragma unroll
+    for (int j = 0; j < NJ; j++) ord[j] = at == j ? 0u : ord[j];
   }
+  fine = !((__ballot(!fine) >> (lane & 48)) & 0xFFFFu);
   double w = 0.0;
-  if (lane < k) w = sigmoid ? 1.0 / (1.0 + exp(-(double)myz)) : exp((double)myz - (double)m) / den;
+  if (rl < k) {
+    const double zs = (double)z[min(mysel, E - 1)];
+    w = sigmoid ? 1.0 / (1.0 + exp(-zs)) : exp(zs - (double)m) / den;
+  }
   if (a.r.norm_topk) {                                                  // (den cancels)
-    const double sum = wave_sum64(w);
+    const double sum = row_sum64(w);
     w = sum == 0.0 ? 0.0 : w / sum;
   }
-  if (lane < k) {
-    a.r.idx[(size_t)t * k + lane] = mysel;
-    a.r.w[(size_t)t * k + lane] = (float)(w * (double)a.r.routed_scale);
+  if (fine && write && rl < k) {
+    a.r.idx[(size_t)t * k + rl] = mysel;
+    a.r.w[(size_t)t * k + rl] = (float)(w * (double)a.r.routed_scale);
   }
-  return true;
+  return fine;
 }
 
-// given logits: one wave per token
-template <int NJ, int SHORT>
+// given logits: four tokens a wave by the short form, what that leaves by the whole wave
+template <int NJ, int LONG>
 __global__ __launch_bounds__(64 * SC_WAVES) void route_scores_kernel(ScoreArgs a, int T) {
   extern __shared__ double sdyn[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = ((int)blockIdx.x * SC_WAVES + wave) * 4;
+  if (t0 >= T) return;
+  const int t = t0 + (lane >> 4);
+  const bool done = select_scores_row<NJ>(a, min(t, T - 1), t < T, lane);
+  const uint64_t left = __ballot(!done && t < T);
+  for (int q = 0; q < 4; q++)
+    if ((left >> (16 * q)) & 1u) select_scores_wave<LONG>(a, t0 + q, a.r.logits + (size_t)(t0 + q) * a.r.E, lane, sdyn + wave * a.r.E);
+}
+// the same by the long form alone, a wave per token
+template <int LONG>
+__global__ __launch_bounds__(64 * SC_WAVES) void route_scores_long_kernel(ScoreArgs a, int T) {
+  extern __shared__ double sdyn[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = (int)blockIdx.x * SC_WAVES + wave;
-  if (t >= T) return;
-  const float* z = a.r.logits + (size_t)t * a.r.E;
-  if constexpr (SHORT > 0)
-    if (select_scores_short<SHORT>(a, t, z, lane)) return;
-  select_scores_wave<NJ>(a, t, z, lane, sdyn + wave * a.r.E);
+  if (t < T) select_scores_wave<LONG>(a, t, a.r.logits + (size_t)t * a.r.E, lane, sdyn + wave * a.r.E);
 }
 
 // router mat-vec of NT tokens by a work-group, as in smoe_route, then one wave per token
@@ -344,16 +362,17 @@ extern "C" int smoe_route_scores(smoe_ctx* ctx, int T, int E, int k, int d_model
     if (!bf16 || T <= 4 * cu) return bf16 ? launch_scores_x<SMOE_BF16, 4>(ctx, a, T) : launch_scores_x<SMOE_F32, 4>(ctx, a, T);
     return launch_scores_x<SMOE_BF16, 8>(ctx, a, T);
   }
-  const int grid = (T + SC_WAVES - 1) / SC_WAVES;
+  // The short form needs rows of 16-byte pieces and groups of whole lanes, a power of two of them up to 8.  With few tokens its longer chain of
+  // instructions counts and not their number: 2047 tokens, 60 experts, top-4 5.4 us, by the long form 3.8; 16384, 256 experts, top-8 23 and 39.
   const size_t lds = n_group > 1 ? (size_t)SC_WAVES * E * 8 : 0;
-  // the short form needs whole lanes in a group, a power of two of them up to 32, and rows that are read 4 NJ bytes at a time
-  const int nj = E <= 64 ? 1 : E <= 128 ? 2 : 4, lpg = E / n_group / nj;
-  const bool brief = E % nj == 0 && (n_group == 1 || (E / n_group % nj == 0 && lpg <= 32 && (lpg & (lpg - 1)) == 0));
-  if (brief && nj == 1) route_scores_kernel<1, 1><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
-  else if (brief && nj == 2) route_scores_kernel<4, 2><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
-  else if (brief) route_scores_kernel<4, 4><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
-  else if (E <= 64) route_scores_kernel<1, 0><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
-  else route_scores_kernel<4, 0><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
+  const int nj = E <= 64 ? 4 : E <= 128 ? 8 : 16, lpg = E / n_group / nj;
+  const bool brief = T > 2048 && E % 4 == 0 && (n_group == 1 || (E / n_group % nj == 0 && (lpg & (lpg - 1)) == 0));
+  const int per = SC_WAVES * (brief ? 4 : 1), grid = (T + per - 1) / per;
+  if (brief && nj == 4) route_scores_kernel<4, 1><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
+  else if (brief && nj == 8) route_scores_kernel<8, 4><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
+  else if (brief) route_scores_kernel<16, 4><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
+  else if (E <= 64) route_scores_long_kernel<1><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
+  else route_scores_long_kernel<4><<<grid, 64 * SC_WAVES, lds, ctx->stream>>>(a, T);
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;
 }

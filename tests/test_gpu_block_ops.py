@@ -54,7 +54,7 @@ def check_route(ctx, z, k, **kw):
         # Each binary64 score carries the exponential's last bit, a sum's and a quotient's: 1 + 1/2 + 1/2 units of 2^-53 relative to a score of at most 1,
         # and half a unit of the sum with the bias.  Two exact values nearer than 2^-51 may come out in either order, or equal.
         s = O.scores(z, kw.get("score", "softmax")) + (0.0 if bias is None else bias.astype(np.float64))
-        assert (np.sort(got, 1)[:, 1:] > np.sort(got, 1)[:, :-1]).all() and kw.get("ng", 1) * (kw.get("gs") == "top2") <= 1
+        assert (np.sort(got, 1)[:, 1:] > np.sort(got, 1)[:, :-1]).all()
         assert np.abs(np.take_along_axis(s, got.astype(np.int64), 1) - np.take_along_axis(s, ri, 1)).max() <= 2.0 ** -51
     close(w, rw, np.abs(rw) * 2 * U32 + 1e-45)             # one rounding from 64 bits, and a subnormal's step
 
@@ -104,7 +104,8 @@ def test_route_scores_ties_masks_and_nan(ctx, score, ng, tg):
 def test_route_scores_close_decisions(ctx, E, ng, tg, gs, k, score):
     """Keys a few units in the last place apart, equal ones, saturated ones: the order is that of the binary64 scores."""
     rng = np.random.default_rng(E + ng)
-    z = np.empty((600, E), np.float32)
+    z = np.empty((2100, E), np.float32)                                              # (from 2049 tokens on fp32 keys decide where they can)
+    z[600:] = rng.standard_normal((1500, E)) * 2
     z[:200] = rng.standard_normal((200, E)) * 2
     z[200:300] = 1.0 + rng.integers(-2, 3, size=(100, E)) * 2.0 ** -23               # neighbours in fp32
     z[300:340] = rng.standard_normal((40, E)) * 1e-12                                 # apart in fp32, scores equal to 1e-12
@@ -113,14 +114,13 @@ def test_route_scores_close_decisions(ctx, E, ng, tg, gs, k, score):
     z[450:500] = np.round(rng.standard_normal((50, E)) * 4) / 4
     z[500:550] = rng.standard_normal((50, E))
     z[500:550][rng.random((50, E)) < 0.4] = -np.inf
-    z[550:] = rng.standard_normal((50, E)) * 1000
+    z[550:600] = rng.standard_normal((50, E)) * 1000
     b = (rng.standard_normal(E) * 0.05).astype(np.float32)
     near = b.copy()
     near[1::2] = near[::2] + np.float32(1e-8)                                         # pairs that a bias sets apart by less than fp32 holds next to 1
     wide = (rng.standard_normal(E) * 30).astype(np.float32)
-    for bias in (None, b, near, wide):
-        for norm in (False, True):
-            check_route(ctx, z, k, score=score, ng=ng, tg=tg, gs=gs, bias=bias, norm=norm)
+    for bias, norm in ((None, False), (None, True), (b, True), (near, False), (wide, False)):
+        check_route(ctx, z, k, score=score, ng=ng, tg=tg, gs=gs, bias=bias, norm=norm)
 
 
 @pytest.mark.parametrize("act", ["f32", "bf16"])

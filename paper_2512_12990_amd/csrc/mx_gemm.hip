@@ -19,15 +19,16 @@ struct MxGemmArgs {
   const uint8_t *wc, *ws, *xc, *xs;
   const int32_t* rows;        // slots, BT for every tile (behind a tile's last slot that slot again), or null: slot i is row i
   const MxTile* tiles;        // null without rows
+  const int* n_tiles;
   void* y;
-  int N, K, n, k, x_slots, x_rows, swiglu, out_f32, col_tiles, max_tiles, super, unit_cols;
+  int N, K, n, k, x_slots, x_rows, swiglu, out_f32, col_tiles, super;
 };
 
 // Work-group e: the slots of expert e, in order, to its tiles of bt.  Every work-group counts all slots, so that none waits
-// for another.  An index outside the experts counts as the nearest of them.  Tiles behind the last one get the count 0.
+// for another.  An index outside the experts counts as the nearest of them.
 //   Bound: one memory round trip and the launch; a thread's slots are fetched sixteen at a time before the first is used (one after the other: 9.9 us for
 // 8192 slots, 60 experts).
-__global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx, int n, int E, int bt, int max_tiles, int32_t* rows, MxTile* tiles) {
+__global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx, int n, int E, int bt, int32_t* rows, MxTile* tiles, int* n_tiles) {
   __shared__ int count[SMOE_MAX_EXPERTS];
   __shared__ int wtot[MG_THREADS / 64];
   __shared__ int last;
@@ -88,8 +89,7 @@ __global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx
   __syncthreads();
   for (int r = cnt + tid; r < nt * bt; r += MG_THREADS) out[r] = last;      // (the expert's last slot fills its last tile)
   for (int i = tid; i < nt; i += MG_THREADS) tiles[t0 + i] = MxTile{e, min(bt, cnt - i * bt)};
-  if (e == E - 1)
-    for (int i = t0 + nt + tid; i < max_tiles; i += MG_THREADS) tiles[i] = MxTile{0, 0};
+  if (e == E - 1 && tid == 0) *n_tiles = t0 + nt;
 }
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -112,37 +112,39 @@ __device__ __forceinline__ void to_lds4(u32x4 rsrc, uint32_t voff, uint32_t soff
 // pieces of a row are stored permuted (piece p at p ^ (row / 2 % 8)), so that sixteen lanes of an operand read, sixteen rows of
 // one piece, fall into different banks.  Half h of a wave multiplies blocks 4h .. 4h + 3 of a stage: its scales of
 // a row are one dword, a byte per step.
+//   What bounds it with many rows is the path from L2 to LDS: 33 - 38 bytes a cycle and CU in pieces of 128 bytes on whole lines with 64 to 96 KB on their way, 22 in pieces of
+// 64 bytes (half lines) or where rows do not begin on lines (K not a multiple of 256).
 //   Scales come 16 bytes a row at a time, two stages' worth: a dword per stage would cost as many requests to L2 as half the codes (dense product,
 // 4096 slots, N 2048, K 10944: 97 us with, 70 us without such loads).
 template <int NT, int NN, int FT, int FN, int NBUF_> struct MgShape {
   static constexpr int NW = NT * NN, BT = 32 * NT * FT, BN = 32 * NN * FN, ROWS = BT + BN, NBUF = NBUF_;
   static constexpr int FRAGS = ROWS / 32, PAIRS = (FRAGS + 1) / 2;
-  static constexpr int LC = ROWS / 8 / NW;                              // code loads of a wave and stage
-  static_assert(ROWS % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0 && PAIRS <= NW && BN % 64 == 0, "whole loads");
+  static constexpr int LCN = BN / 8 / NW, LCT = BT / 8 / NW, LC = LCN + LCT;      // code loads of a wave and stage
+  static_assert(BN % (8 * NW) == 0 && BT % (8 * NW) == 0 && NW % 2 == 0 && PAIRS <= NW && BN % 64 == 0 && BT <= 64 * NW && (NBUF == 2 || NBUF == 3), "whole loads");
   static constexpr int codes = ROWS * 128, scales = PAIRS * 1024, extra = PAIRS * 256;      // a code buffer; one of two scale buffers; a fifth dword for each row
   static constexpr int chunk(bool unal) { return scales + (unal ? extra : 0); }
   static constexpr int slots_at(bool unal) { return NBUF * codes + 2 * chunk(unal); }       // where the tile's slots stand
   static constexpr int lds(bool unal) { return slots_at(unal) + BT * 4; }
-  static constexpr int out_row = BN * 4 + 16;                           // epilogue: bytes of a row (fp32 at most; the 16 keep the rows of a fragment in different banks)
-  static_assert(32 * NT * out_row <= NBUF * codes, "a fragment row of the result fits the code buffers");
+  static constexpr int out_row = 128 + 16, out_wave = 32 * out_row;                         // result: a wave's place to turn its fragments round (16 bytes of padding keep the rows in different banks)
+  static_assert(NW * out_wave <= NBUF * codes, "the results fit the code buffers");
 };
 
 // UNAL: a row's scales do not begin on a dword (K not a multiple of 128): a fifth dword is fetched, and scales are shifted.
 template <class S, bool UNAL, int NT, int NN, int FT, int FN>
 __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
-  constexpr int NW = S::NW, BT = S::BT, BN = S::BN, NBUF = S::NBUF, LC = S::LC;
-  constexpr int LCN = BN / 8 / NW, LCT = LC - LCN;                      // code loads of weight rows, of token rows
+  constexpr int NW = S::NW, BT = S::BT, BN = S::BN, NBUF = S::NBUF, LC = S::LC, LCN = S::LCN, LCT = S::LCT;
   constexpr uint32_t STAGE = S::codes, SCALES = NBUF * STAGE, CHUNK = S::chunk(UNAL);
+  constexpr uint32_t NONE = 0x80000000u;                               // beyond every buffer: nothing is fetched
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
-  // ---- which tile.  A unit, `super` tiles of slots side by side for each of `unit_cols` tiles of weight rows, is consecutive work-groups of one XCD, whose
-  // L2 then serves the rows they share; units go round the XCDs.  All of it is known without a look at memory, so that the tile's record and its
-  // slots are fetched together.
-  const int per_unit = a.super * a.unit_cols, chunks = (a.col_tiles + a.unit_cols - 1) / a.unit_cols;
-  const int place = (int)blockIdx.x >> 3, unit = (place / per_unit) * 8 + ((int)blockIdx.x & 7), in_unit = place % per_unit;
-  const int ct = unit % chunks * a.unit_cols + in_unit / a.super, ti = unit / chunks * a.super + in_unit % a.super;
-  if (ct >= a.col_tiles) return;
-  if (ti >= a.max_tiles) return;
+  // ---- which tile.  Consecutive items, `super` tiles of slots side by side for every tile of weight rows, stay on one XCD, whose L2 then serves the rows
+  // they share
+  const int n_tiles = a.rows ? uni(*a.n_tiles) : (a.n + BT - 1) / BT;
+  const int n_items = n_tiles * a.col_tiles, run = (n_items + 7) >> 3;
+  const int place = (int)blockIdx.x >> 3, item = ((int)blockIdx.x & 7) * run + place;
+  if (place >= run || item >= n_items) return;
+  const int per_band = a.super * a.col_tiles, band = uni(item / per_band), in_band = item - band * per_band;
+  const int band_n = min(a.super, n_tiles - band * a.super), ct = uni(in_band / band_n), ti = band * a.super + in_band - ct * band_n;
   MxTile tile;
   if (a.rows) {
     tile = a.tiles[ti];
@@ -151,7 +153,7 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
     tile = MxTile{0, min(BT, a.n - ti * BT)};
   }
   const int32_t* tile_rows = a.rows + (size_t)ti * BT;
-  const int nb = a.K >> 5, n0 = ct * BN, n_st = (nb + 7) >> 3;
+  const int nb = a.K >> 5, n0 = ct * BN, n_st = (nb + 7) >> 3, n_full = nb >> 3;
   const uint32_t rowb = (uint32_t)(a.K >> 1);
   const u32x4 rwc = buffer_of(a.wc + (size_t)tile.expert * a.N * rowb, (uint32_t)a.N * rowb);
   const u32x4 rws = buffer_of(a.ws + (size_t)tile.expert * a.N * nb, (uint32_t)a.N * (uint32_t)nb);
@@ -159,17 +161,15 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   const u32x4 rxs = buffer_of(a.xs, ((uint32_t)a.x_rows * (uint32_t)nb + 3u) & ~3u);      // (whole dwords: every one fetched holds a byte of the array)
   auto slot_of = [&](int r) { return a.rows ? tile_rows[r] : ti * BT + min(r, tile.count - 1); };
   auto x_row = [&](int r) { const int slot = slot_of(r); return (uint32_t)(a.x_slots ? slot : slot / a.k); };      // row of X of the tile's slot r
-  int* slots = (int*)(As + S::slots_at(UNAL));                          // for the epilogue
+  int* slots = (int*)(As + S::slots_at(UNAL));                          // for the result
   if (tid < BT) slots[tid] = slot_of(tid);
-  // ---- addresses.  Code load q of a wave: rows 8 (NW q + wave) .. + 7 of the stage, weight rows first; a lane's piece is the same for all q
-  constexpr uint32_t NONE = 0x80000000u;                               // beyond every buffer: nothing is fetched
+  // ---- addresses.  Code load q of a wave: rows 8 (NW q + wave) .. + 7 of the weight rows, then of the token rows; a lane's piece is the same for all q
   const int pr = lane >> 3, piece = (lane & 7) ^ (((8 * wave + pr) >> 1) & 7);
   const uint32_t wv = (uint32_t)(n0 + 8 * wave + pr) * rowb + piece * 16u;
-  uint32_t xv[LCT > 0 ? LCT : 1];
+  uint32_t xv[LCT];
 #pragma unroll
   for (int q = 0; q < LCT; q++) xv[q] = x_row(8 * (NW * q + wave) + pr) * rowb + piece * 16u;
   const bool piece_last = (n_st - 1) * 8 + piece < nb;                 // the lane's piece exists in the last stage
-  if (tile.count == 0) return;                                         // (uniform)
   // scale loads: wave w brings fragments 2p and 2p + 1, p = w (or a copy of an earlier pair), a row a lane
   const int pair = wave % S::PAIRS, sf = 2 * pair + h;
   const bool of_w = pair < BN / 64;
@@ -179,19 +179,18 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   const uint32_t as_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)As;
   // code loads q0 .. q1 - 1 of the LC that bring stage st into a buffer (past the last stage nothing is fetched, but the load counts)
   auto issue = [&](int st, uint32_t buf, int q0, int q1) __attribute__((always_inline)) {
-    const uint32_t lds = as_base + buf;
     const bool skip = st >= n_st || (st == n_st - 1 && !piece_last);
 #pragma unroll
     for (int q = q0; q < q1; q++)
-      to_lds16(q < LCN ? rwc : rxc, skip ? NONE : q < LCN ? wv + (uint32_t)(8 * NW * q) * rowb : xv[q < LCN ? 0 : q - LCN], (uint32_t)st * 128u, lds + (NW * q + wave) * 1024u);
+      to_lds16(q < LCN ? rwc : rxc, skip ? NONE : q < LCN ? wv + (uint32_t)(8 * NW * q) * rowb : xv[q < LCN ? 0 : q - LCN], (uint32_t)st * 128u, as_base + buf + (NW * q + wave) * 1024u);
   };
   constexpr int LSC = UNAL ? 2 : 1;
   // scales of stages 2g and 2g + 1.  A 16-byte load may run over the row's end (into the next row, or zeros behind the array)
   auto issue_scales = [&](int g) __attribute__((always_inline)) {
-    const uint32_t lds = as_base + SCALES + (g & 1) * CHUNK + pair * 1024u;
+    const uint32_t lds = as_base + SCALES + (g & 1) * CHUNK;
     const int left = nb - 16 * g;                                      // the row's blocks from this chunk on
-    to_lds16(rs, left <= 0 ? NONE : sv & ~3u, (uint32_t)g * 16u, lds);
-    if (UNAL) to_lds4(rs, left + (int)(sv & 3u) <= 16 ? NONE : (sv & ~3u) + 16u, (uint32_t)g * 16u, as_base + SCALES + (g & 1) * CHUNK + S::scales + pair * 256u);
+    to_lds16(rs, left <= 0 ? NONE : sv & ~3u, (uint32_t)g * 16u, lds + pair * 1024u);
+    if (UNAL) to_lds4(rs, left + (int)(sv & 3u) <= 16 ? NONE : (sv & ~3u) + 16u, (uint32_t)g * 16u, lds + S::scales + pair * 256u);
   };
   const int wt = wave % NT, wn = wave / NT;
   f32x16 acc[FN][FT];
@@ -217,8 +216,14 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
     const uint32_t hi = *(const uint32_t*)(at + (d == 3 ? (uint32_t)(S::scales + f * 128 + c * 4) : o + 4));
     return (uint32_t)__builtin_amdgcn_alignbyte(hi, lo, sh);
   };
-  const uint32_t swz = (uint32_t)((c >> 1) & 7);
+  auto read_scales = [&](int st, uint32_t (&sw)[FN], uint32_t (&sx)[FT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FN; i++) sw[i] = scale_of(st, wn * FN + i, h, shw[i]);
+#pragma unroll
+    for (int j = 0; j < FT; j++) sx[j] = scale_of(st, BN / 32 + wt * FT + j, h, shx[j]);
+  };
   struct Frags { u32x4 w[FN], x[FT]; };
+  const uint32_t swz = (uint32_t)((c >> 1) & 7);
   auto read = [&](const uint8_t* st, int p, Frags& f) __attribute__((always_inline)) {
     const uint32_t o = c * 128 + (((uint32_t)p ^ swz) * 16);
 #pragma unroll
@@ -243,25 +248,15 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   const std::integral_constant<int, 1> s1{};
   const std::integral_constant<int, 2> s2{};
   const std::integral_constant<int, 3> s3{};
-  auto read_scales = [&](int st, uint32_t (&sw)[FN], uint32_t (&sx)[FT]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < FN; i++) sw[i] = scale_of(st, wn * FN + i, h, shw[i]);
-#pragma unroll
-    for (int j = 0; j < FT; j++) sx[j] = scale_of(st, BN / 32 + wt * FT + j, h, shx[j]);
-  };
-  // ---- columns.  The operands of a step are read while the one before it is multiplied; in front of a stage's last step comes the
-  // barrier behind which the stage has been read by all and the next one is there.  The LC loads into the buffer so freed are dealt to the
-  // products of the following steps: a direct load keeps the texture path busy for some 22 cycles, and eight waves that send
-  // all theirs at once stand still meanwhile.  With two buffers the loads go to three of the four steps, so that the last of them has a step's time.
-  constexpr int QS = NBUF == 2 ? 3 : 4;
-  constexpr int HEAD = LC / QS;                                        // loads dealt to the step behind the barrier
-  constexpr int M = FN * FT;
+  // ---- columns.  The operands of a step are read while the one before it is multiplied.  In front of a stage's last step comes the barrier behind which the stage
+  // has been read by all and the next one is there.  The loads into the buffer so freed: with two buffers (and another work-group on the CU) at
+  // once, to be as long on their way as they can be; with three dealt to the products of the next four steps, since eight waves that send all theirs at once
+  // stand still meanwhile (a direct load keeps the texture path busy for some 22 cycles).
+  constexpr int M = FN * FT, HEAD = NBUF == 2 ? LC : LC / 4;
   auto deal = [&](int st, uint32_t buf, int quarter, int m) __attribute__((always_inline)) {
-    if (quarter >= QS) return;
-    const int q0 = LC * quarter / QS, n = LC * (quarter + 1) / QS - q0;
-    issue(st, buf, q0 + n * m / M, q0 + n * (m + 1) / M);
+    const int q0 = LC * quarter / 4, n = LC * (quarter + 1) / 4 - q0;
+    if (NBUF > 2) issue(st, buf, q0 + n * m / M, q0 + n * (m + 1) / M);
   };
-  const int n_full = nb >> 3;
   issue_scales(0);
   issue_scales(1);
 #pragma unroll
@@ -292,9 +287,10 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
     if (NBUF > 2 && (st & 1) == 0 && st > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC + LSC) : "memory");
     else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC) : "memory");
     uint32_t nw[FN], nx[FT];
-    read_scales(st + 1, nw, nx);
+    read_scales(st + 1, nw, nx);                                       // (behind the last stage: what is read is not used)
     read(As + next, 4 * h, f0);
     __builtin_amdgcn_sched_barrier(0);
+    if (NBUF == 2) issue(st + NBUF, cur, 0, LC);
     mul(s3, f1, sw, sx, [&](int m) __attribute__((always_inline)) { deal(st + NBUF, cur, 0, m); });
     if (st & 1) issue_scales(((st + 1) >> 1) + 1);
 #pragma unroll
@@ -328,38 +324,45 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
       for (int j = 0; j < FT; j++) sx[j] >>= 8;
     }
   }
-  // ---- result.  Lane: slot c of a fragment, weight rows 8 (r / 4) + 4 h + r % 4.  A row of fragments at a time goes through LDS, so that
-  // whole lines of Y are written (stores of 4 or 8 bytes straight from the lanes: 22 of 96 us, 2048 tokens, top-4 of 60, N 2816, K 2048).
+  // (no load is on its way to LDS any more, and every wave has read its operands)
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  // ---- result.  Lane: slot c of a fragment, weight rows 8 (r / 4) + 4 h + r % 4.  A wave turns its fragments round in LDS of its own, so that it writes 64 or
+  // 128 neighbouring bytes of a row of Y (32 with one fragment; stores of 4 or 8 bytes straight from the lanes: 22 of 96 us, 2048 tokens, top-4 of 60, N 2816, K 2048).
   const int osz = a.out_f32 ? 4 : 2, sg = a.swiglu;
-  const int row_n = (sg ? BN >> 1 : BN), n_out = sg ? a.N >> 1 : a.N, c0 = sg ? n0 >> 1 : n0;      // columns of the tile's rows, of Y, the tile's first
-  const int lpr = 31 - __builtin_clz((unsigned)(row_n * osz / 16));                                // log2 of a row's 16-byte pieces
+  const int n_out = sg ? a.N >> 1 : a.N, per_pass = a.out_f32 && !sg ? 1 : FN;                     // columns of Y; fragments at a time
+  const int lpr = 31 - __builtin_clz((unsigned)(per_pass * (sg ? 16 : 32) * osz / 16));           // log2 of a row's 16-byte pieces
+  uint8_t* o = As + wave * S::out_wave;
 #pragma unroll
   for (int j = 0; j < FT; j++) {
-    // (the first time: no load is on its way to LDS any more, and every wave has read its operands)
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(0) : "memory");
-    if (FT > 1 && j * 32 >= tile.count) break;                          // (no wave has slots in these rows)
-    uint8_t* o = As + (wt * 32 + c) * S::out_row;
+    const int r0 = (wt * FT + j) * 32;
+    if (r0 >= tile.count) continue;
 #pragma unroll
-    for (int i = 0; i < FN; i++)
+    for (int i = 0; i < FN; i++) {
+      const int ip = per_pass == 1 ? 0 : i;                            // place of the fragment in the pass
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int nr = (wn * FN + i) * 32 + 2 * r + 4 * h;
+        const int nr = ip * 32 + 2 * r + 4 * h;
         const float v0 = acc[i][j][r], v1 = acc[i][j][r + 1], v2 = acc[i][j][r + 2], v3 = acc[i][j][r + 3];
+        uint8_t* to = o + c * S::out_row;
         if (sg) {
           const float o0 = swiglu(v0, v1), o1 = swiglu(v2, v3);
-          if (a.out_f32) *(float2*)(o + (nr >> 1) * 4) = make_float2(o0, o1);
-          else *(uint32_t*)(o + (nr >> 1) * 2) = pack_bf16_rne(o0, o1);
+          if (a.out_f32) *(float2*)(to + (nr >> 1) * 4) = make_float2(o0, o1);
+          else *(uint32_t*)(to + (nr >> 1) * 2) = pack_bf16_rne(o0, o1);
         } else {
-          if (a.out_f32) *(float4*)(o + nr * 4) = make_float4(v0, v1, v2, v3);
-          else *(uint2*)(o + nr * 2) = make_uint2(pack_bf16_rne(v0, v1), pack_bf16_rne(v2, v3));
+          if (a.out_f32) *(float4*)(to + nr * 4) = make_float4(v0, v1, v2, v3);
+          else *(uint2*)(to + nr * 2) = make_uint2(pack_bf16_rne(v0, v1), pack_bf16_rne(v2, v3));
         }
       }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    for (int x = tid; x < (32 * NT) << lpr; x += 64 * NW) {
-      const int lr = x >> lpr, p = x & ((1 << lpr) - 1);
-      const int tr = ((lr >> 5) * FT + j) * 32 + (lr & 31), col = c0 + p * (16 / osz);
-      if (tr < tile.count && col < n_out)                              // (N is a multiple of 16: sixteen bytes are in or out)
-        *(uint4*)((uint8_t*)a.y + ((size_t)slots[tr] * n_out + col) * osz) = *(const uint4*)(As + lr * S::out_row + p * 16);
+      if (ip == per_pass - 1) {
+        asm volatile("" ::: "memory");                                 // (LDS keeps a wave's accesses in order; so does the compiler now)
+        const int col0 = (n0 + (wn * FN + i - ip) * 32) >> sg;
+        for (int x = lane; x < 32 << lpr; x += 64) {
+          const int tr = x >> lpr, p = x & ((1 << lpr) - 1), col = col0 + p * (16 / osz);
+          if (r0 + tr < tile.count && col < n_out)                     // (N is a multiple of 16: sixteen bytes are in or out)
+            *(uint4*)((uint8_t*)a.y + ((size_t)slots[r0 + tr] * n_out + col) * osz) = *(const uint4*)(o + tr * S::out_row + p * 16);
+        }
+        asm volatile("" ::: "memory");
+      }
     }
   }
 }
@@ -373,7 +376,7 @@ __global__ __launch_bounds__(64 * NT * NN) void mx_gemm_kernel(MxGemmArgs a) {
 static inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct MxShape { int bt, bn; };
-static const MxShape g_shapes[4] = {{32, 128}, {64, 128}, {128, 128}, {128, 256}};
+static const MxShape g_shapes[5] = {{32, 128}, {64, 128}, {128, 128}, {128, 256}, {256, 256}};
 static int pick_shape(int n, int E, int N) {
   if (const char* f = getenv("MXS")) return atoi(f);
   const int per = n / E;
@@ -382,11 +385,11 @@ static int pick_shape(int n, int E, int N) {
 
 template <bool UNAL, int NT, int NN, int FT, int FN, int NBUF>
 static int launch_gemm_t(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int slot) {
-  const size_t lds = MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL);
-  static_assert(MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL) <= 160 * 1024, "LDS");
+  constexpr int lds = MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL);
+  static_assert(lds <= 160 * 1024, "LDS");
   size_t& granted = ctx->mx_lds_granted[slot * 2 + UNAL];
-  if (lds > 64u * 1024u && granted < lds) {      // once per context: beyond the default 64 KB
-    HIPCHK(ctx, hipFuncSetAttribute((const void*)mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  if (lds > 64 * 1024 && granted < (size_t)lds) {      // once per context: beyond the default 64 KB
+    HIPCHK(ctx, hipFuncSetAttribute((const void*)mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     granted = lds;
   }
   mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF><<<grid, 64 * NT * NN, lds, ctx->stream>>>(a);
@@ -398,7 +401,7 @@ static int launch_gemm(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int sl
   return (a.K >> 5) % 4 ? launch_gemm_t<true, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot) : launch_gemm_t<false, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot);
 }
 
-struct MxProductLayout { size_t rows, tiles, total; };
+struct MxProductLayout { size_t rows, tiles, n_tiles, total; };
 static int max_tiles_of(int n, int E, int bt) { return n / bt + (n < E ? n : E); }
 static MxProductLayout product_layout(int T, int k, int E) {
   MxProductLayout l;
@@ -411,7 +414,8 @@ static MxProductLayout product_layout(int T, int k, int E) {
   }
   l.rows = 0;
   l.tiles = up256(rows * 4);
-  l.total = l.tiles + up256(tiles * sizeof(MxTile)) + 256;
+  l.n_tiles = l.tiles + up256(tiles * sizeof(MxTile));
+  l.total = l.n_tiles + 256;
   return l;
 }
 
@@ -444,34 +448,28 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
   ON_DEVICE_OF(ctx);
   const int n = T * k;
   uint8_t* s = (uint8_t*)scratch_dev;
-  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, y_dev, N, K, n, k, x_slots, T * (x_slots ? k : 1), swiglu,
-               out_dtype == SMOE_F32, 0, 0, 1, 1};
+  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, y_dev, N, K, n, k, x_slots, T * (x_slots ? k : 1),
+               swiglu, out_dtype == SMOE_F32, 0, 1};
   const int shape = pick_shape(n, E, N);
   const int bt = g_shapes[shape].bt;
   a.col_tiles = (N + g_shapes[shape].bn - 1) / g_shapes[shape].bn;
-  a.max_tiles = (n + bt - 1) / bt;
-  a.super = a.max_tiles / E < 1 ? 1 : a.max_tiles / E > 8 ? 8 : a.max_tiles / E;
+  int max_tiles = (n + bt - 1) / bt;
+  a.super = max_tiles / E < 1 ? 1 : max_tiles / E > 8 ? 8 : max_tiles / E;
   if (idx_dev) {
     int32_t* rows = (int32_t*)(s + l.rows);
     MxTile* tiles = (MxTile*)(s + l.tiles);
-    a.max_tiles = max_tiles_of(n, E, bt);
-    mx_group_kernel<<<E, MG_THREADS, 0, ctx->stream>>>(idx_dev, n, E, bt, a.max_tiles, rows, tiles);
+    int* n_tiles = (int*)(s + l.n_tiles);
+    max_tiles = max_tiles_of(n, E, bt);
+    mx_group_kernel<<<E, MG_THREADS, 0, ctx->stream>>>(idx_dev, n, E, bt, rows, tiles, n_tiles);
     HIPCHK(ctx, hipGetLastError());
-    a.rows = rows; a.tiles = tiles;
+    a.rows = rows; a.tiles = tiles; a.n_tiles = n_tiles;
   }
-  // columns of a unit: as many as still share the tiles (of experts whose last one is half full) out to the XCDs to within 3 % of evenly
-  const int bands = (a.max_tiles + a.super - 1) / a.super;
-  const long long tiles = idx_dev ? n / bt + (n < E ? n : E + 1) / 2 : a.max_tiles, used = (tiles + a.super - 1) / a.super;
-  unsigned grid = 0;
-  for (a.unit_cols = a.col_tiles;; a.unit_cols = (a.unit_cols + 1) / 2) {
-    const long long chunks = (a.col_tiles + a.unit_cols - 1) / a.unit_cols, per_unit = (long long)a.super * a.unit_cols;
-    grid = (unsigned)((bands * chunks + 7) / 8 * per_unit * 8);
-    if (a.unit_cols == 1 || (used * chunks + 7) / 8 * per_unit * 800 <= 103 * tiles * a.col_tiles) break;
-  }
+  const unsigned grid = ((unsigned)max_tiles * (unsigned)a.col_tiles + 7) / 8 * 8;
   switch (shape) {
     case 0: return launch_gemm<1, 4, 1, 1, 3>(ctx, a, grid, 0);
     case 1: return launch_gemm<2, 2, 1, 2, 3>(ctx, a, grid, 1);
     case 2: return launch_gemm<2, 2, 2, 2, 2>(ctx, a, grid, 2);
-    default: return launch_gemm<2, 4, 2, 2, 3>(ctx, a, grid, 3);
+    case 3: return launch_gemm<2, 4, 2, 2, 3>(ctx, a, grid, 3);
+    default: return launch_gemm<2, 4, 4, 2, 2>(ctx, a, grid, 4);
   }
 }

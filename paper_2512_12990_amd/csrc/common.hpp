@@ -48,7 +48,7 @@ struct smoe_ctx {
   size_t down_lds_granted[60];   // dynamic LDS already granted to each down_kernel instantiation on this device
   size_t gemm_lds_granted[60];   // likewise for the instantiations of grouped_gemm_kernel
   size_t route_lds_granted[8];   // likewise for the instantiations of route_batch_kernel
-  size_t mx_lds_granted[10];     // likewise for the instantiations of mx_gemm_kernel
+  size_t mx_lds_granted[6];     // likewise for the instantiations of mx_gemm_kernel
   // single-launch decode (smoe_ctx_single_launch)
   int one_launch;                // the mode is on
   int one_spin_limit;            // polls before a work-group gives up waiting for the others

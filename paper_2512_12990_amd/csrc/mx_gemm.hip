@@ -4,7 +4,6 @@
 //   gemm     a work-group per tile of slots and BN weight rows
 #include "mx.hpp"
 #include <type_traits>
-#include <stdlib.h>
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -108,7 +107,7 @@ __device__ __forceinline__ void to_lds4(u32x4 rsrc, uint32_t voff, uint32_t soff
 }
 
 // Shape of a work-group: NT waves along the slots times NN along the weight rows, FT by FN fragments of 32 a wave.
-//   A stage is 256 columns, 128 bytes of codes a row, brought straight into one of NBUF buffers.  The eight 16-byte
+//   A stage is 256 columns, 128 bytes of codes a row, brought straight into one of three buffers.  The eight 16-byte
 // pieces of a row are stored permuted (piece p at p ^ (row / 2 % 8)), so that sixteen lanes of an operand read, sixteen rows of
 // one piece, fall into different banks.  Half h of a wave multiplies blocks 4h .. 4h + 3 of a stage: its scales of
 // a row are one dword, a byte per step.
@@ -116,11 +115,11 @@ __device__ __forceinline__ void to_lds4(u32x4 rsrc, uint32_t voff, uint32_t soff
 // 64 bytes (half lines) or where rows do not begin on lines (K not a multiple of 256).
 //   Scales come 16 bytes a row at a time, two stages' worth: a dword per stage would cost as many requests to L2 as half the codes (dense product,
 // 4096 slots, N 2048, K 10944: 97 us with, 70 us without such loads).
-template <int NT, int NN, int FT, int FN, int NBUF_> struct MgShape {
-  static constexpr int NW = NT * NN, BT = 32 * NT * FT, BN = 32 * NN * FN, ROWS = BT + BN, NBUF = NBUF_;
+template <int NT, int NN, int FT, int FN> struct MgShape {
+  static constexpr int NW = NT * NN, BT = 32 * NT * FT, BN = 32 * NN * FN, ROWS = BT + BN, NBUF = 3;
   static constexpr int FRAGS = ROWS / 32, PAIRS = (FRAGS + 1) / 2;
   static constexpr int LCN = BN / 8 / NW, LCT = BT / 8 / NW, LC = LCN + LCT;      // code loads of a wave and stage
-  static_assert(BN % (8 * NW) == 0 && BT % (8 * NW) == 0 && NW % 2 == 0 && PAIRS <= NW && BN % 64 == 0 && BT <= 64 * NW && (NBUF == 2 || NBUF == 3), "whole loads");
+  static_assert(BN % (8 * NW) == 0 && BT % (8 * NW) == 0 && NW % 2 == 0 && PAIRS <= NW && BN % 64 == 0 && BT <= 64 * NW, "whole loads");
   static constexpr int codes = ROWS * 128, scales = PAIRS * 1024, extra = PAIRS * 256;      // a code buffer; one of two scale buffers; a fifth dword for each row
   static constexpr int chunk(bool unal) { return scales + (unal ? extra : 0); }
   static constexpr int slots_at(bool unal) { return NBUF * codes + 2 * chunk(unal); }       // where the tile's slots stand
@@ -249,20 +248,19 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   const std::integral_constant<int, 2> s2{};
   const std::integral_constant<int, 3> s3{};
   // ---- columns.  The operands of a step are read while the one before it is multiplied.  In front of a stage's last step comes the barrier behind which the stage
-  // has been read by all and the next one is there.  The loads into the buffer so freed: with two buffers (and another work-group on the CU) at
-  // once, to be as long on their way as they can be; with three dealt to the products of the next four steps, since eight waves that send all theirs at once
-  // stand still meanwhile (a direct load keeps the texture path busy for some 22 cycles).
-  constexpr int M = FN * FT, HEAD = NBUF == 2 ? LC : LC / 4;
+  // has been read by all and the next one is there.  The loads into the buffer so freed are dealt to the products of the next four steps: a direct load keeps the texture
+  // path busy for some 22 cycles, and eight waves that send all theirs at once stand still meanwhile.
+  constexpr int M = FN * FT, HEAD = LC / 4;
   auto deal = [&](int st, uint32_t buf, int quarter, int m) __attribute__((always_inline)) {
     const int q0 = LC * quarter / 4, n = LC * (quarter + 1) / 4 - q0;
-    if (NBUF > 2) issue(st, buf, q0 + n * m / M, q0 + n * (m + 1) / M);
+    issue(st, buf, q0 + n * m / M, q0 + n * (m + 1) / M);
   };
   issue_scales(0);
   issue_scales(1);
 #pragma unroll
   for (int st = 0; st < NBUF - 1; st++) issue(st, st * STAGE, 0, LC);
   issue(NBUF - 1, (NBUF - 1) * STAGE, 0, HEAD);
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC + HEAD) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LC + HEAD) : "memory");
   uint32_t cur = 0, before = (NBUF - 1) * STAGE;                       // buffer of the stage, and of the one before it
   uint32_t sw[FN], sx[FT];
   Frags f0, f1;
@@ -283,14 +281,13 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
     read(at, 4 * h + 3, f1);
     __builtin_amdgcn_sched_barrier(0);
     mul(s2, f0, sw, sx, [&](int m) __attribute__((always_inline)) { deal(ahead, before, 3, m); });
-    // younger than stage st + 1: NBUF - 2 stages of codes, and with three buffers the scales sent for behind an odd stage
-    if (NBUF > 2 && (st & 1) == 0 && st > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC + LSC) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NBUF - 2) * LC) : "memory");
+    // younger than stage st + 1: a stage of codes and the scales sent for behind an odd stage
+    if ((st & 1) == 0 && st > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LC + LSC) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LC) : "memory");
     uint32_t nw[FN], nx[FT];
     read_scales(st + 1, nw, nx);                                       // (behind the last stage: what is read is not used)
     read(As + next, 4 * h, f0);
     __builtin_amdgcn_sched_barrier(0);
-    if (NBUF == 2) issue(st + NBUF, cur, 0, LC);
     mul(s3, f1, sw, sx, [&](int m) __attribute__((always_inline)) { deal(st + NBUF, cur, 0, m); });
     if (st & 1) issue_scales(((st + 1) >> 1) + 1);
 #pragma unroll
@@ -367,38 +364,49 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   }
 }
 
-template <bool UNAL, int NT, int NN, int FT, int FN, int NBUF>
+template <bool UNAL, int NT, int NN, int FT, int FN>
 __global__ __launch_bounds__(64 * NT * NN) void mx_gemm_kernel(MxGemmArgs a) {
   extern __shared__ __align__(1024) uint8_t mdyn[];
-  mx_gemm_tile<MgShape<NT, NN, FT, FN, NBUF>, UNAL, NT, NN, FT, FN>(a, mdyn);
+  mx_gemm_tile<MgShape<NT, NN, FT, FN>, UNAL, NT, NN, FT, FN>(a, mdyn);
 }
 
 static inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-struct MxShape { int bt, bn; };
-static const MxShape g_shapes[5] = {{32, 128}, {64, 128}, {128, 128}, {128, 256}, {256, 256}};
-static int pick_shape(int n, int E, int N) {
-  if (const char* f = getenv("MXS")) return atoi(f);
-  const int per = n / E;
-  return per <= 24 ? 0 : per <= 64 ? 1 : 3;
+// The tile shapes: slots, weight rows, work-groups that fit a CU, and a work-group's time with all of those filled, relative to the first shape's (dense,
+// 4096 x 8192 x 8192: 320 / 214 / 162 us in 16 / 8 / 4 rounds).
+struct MxShape { int bt, bn, per_cu; double cost; };
+static const MxShape g_shapes[3] = {{32, 128, 2, 1.0}, {64, 128, 2, 1.34}, {128, 256, 1, 2.1}};
+// tiles of bt slots: experts' last ones are taken to be half full
+static long long likely_tiles(int n, int E, int bt) { return E == 1 ? (n + bt - 1) / bt : n / bt + (n < E ? n : E + 1) / 2; }
+// The shape with the least rounds of work-groups times their cost; one round at least.  Microseconds of shapes 0 / 1 / 2 (top-6 of 64, N 2816, K 2048): 100
+// tokens 39.0 / 39.3 / 45.3, 300 47.2 / 44.4 / 53.1, 800 75.8 / 61.9 / 66.6, 1500 118 / 87.7 / 82.2; dense, N 2048, K 2048: 256 rows 6.1 / 7.5 / 11.7, 4096 28.2 / 21.0 / 16.9.
+static int pick_shape(int n, int E, int N, int n_cu) {
+  int best = 0;
+  double least = 0.0;
+  for (int i = 0; i < 3; i++) {
+    const MxShape& s = g_shapes[i];
+    const double rounds = (double)likely_tiles(n, E, s.bt) * ((N + s.bn - 1) / s.bn) / ((double)s.per_cu * n_cu), t = (rounds > 1.0 ? rounds : 1.0) * s.cost;
+    if (i == 0 || t < least) { best = i; least = t; }
+  }
+  return best;
 }
 
-template <bool UNAL, int NT, int NN, int FT, int FN, int NBUF>
+template <bool UNAL, int NT, int NN, int FT, int FN>
 static int launch_gemm_t(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int slot) {
-  constexpr int lds = MgShape<NT, NN, FT, FN, NBUF>::lds(UNAL);
+  constexpr int lds = MgShape<NT, NN, FT, FN>::lds(UNAL);
   static_assert(lds <= 160 * 1024, "LDS");
   size_t& granted = ctx->mx_lds_granted[slot * 2 + UNAL];
   if (lds > 64 * 1024 && granted < (size_t)lds) {      // once per context: beyond the default 64 KB
-    HIPCHK(ctx, hipFuncSetAttribute((const void*)mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    HIPCHK(ctx, hipFuncSetAttribute((const void*)mx_gemm_kernel<UNAL, NT, NN, FT, FN>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     granted = lds;
   }
-  mx_gemm_kernel<UNAL, NT, NN, FT, FN, NBUF><<<grid, 64 * NT * NN, lds, ctx->stream>>>(a);
+  mx_gemm_kernel<UNAL, NT, NN, FT, FN><<<grid, 64 * NT * NN, lds, ctx->stream>>>(a);
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;
 }
-template <int NT, int NN, int FT, int FN, int NBUF>
+template <int NT, int NN, int FT, int FN>
 static int launch_gemm(smoe_ctx* ctx, const MxGemmArgs& a, unsigned grid, int slot) {
-  return (a.K >> 5) % 4 ? launch_gemm_t<true, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot) : launch_gemm_t<false, NT, NN, FT, FN, NBUF>(ctx, a, grid, slot);
+  return (a.K >> 5) % 4 ? launch_gemm_t<true, NT, NN, FT, FN>(ctx, a, grid, slot) : launch_gemm_t<false, NT, NN, FT, FN>(ctx, a, grid, slot);
 }
 
 struct MxProductLayout { size_t rows, tiles, n_tiles, total; };
@@ -450,7 +458,7 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
   uint8_t* s = (uint8_t*)scratch_dev;
   MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, y_dev, N, K, n, k, x_slots, T * (x_slots ? k : 1),
                swiglu, out_dtype == SMOE_F32, 0, 1};
-  const int shape = pick_shape(n, E, N);
+  const int shape = pick_shape(n, E, N, ctx->n_cu);
   const int bt = g_shapes[shape].bt;
   a.col_tiles = (N + g_shapes[shape].bn - 1) / g_shapes[shape].bn;
   int max_tiles = (n + bt - 1) / bt;
@@ -465,11 +473,7 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
     a.rows = rows; a.tiles = tiles; a.n_tiles = n_tiles;
   }
   const unsigned grid = ((unsigned)max_tiles * (unsigned)a.col_tiles + 7) / 8 * 8;
-  switch (shape) {
-    case 0: return launch_gemm<1, 4, 1, 1, 3>(ctx, a, grid, 0);
-    case 1: return launch_gemm<2, 2, 1, 2, 3>(ctx, a, grid, 1);
-    case 2: return launch_gemm<2, 2, 2, 2, 2>(ctx, a, grid, 2);
-    case 3: return launch_gemm<2, 4, 2, 2, 3>(ctx, a, grid, 3);
-    default: return launch_gemm<2, 4, 4, 2, 2>(ctx, a, grid, 4);
-  }
+  if (shape == 0) return launch_gemm<1, 4, 1, 1>(ctx, a, grid, 0);
+  if (shape == 1) return launch_gemm<2, 2, 1, 2>(ctx, a, grid, 1);
+  return launch_gemm<2, 4, 2, 2>(ctx, a, grid, 2);
 }

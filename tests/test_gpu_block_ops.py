@@ -316,6 +316,25 @@ def test_mx_product_exact(ctx, T, k, E, N, K, how, slots):
         close(got, want, np.abs(want) * (8 * U32 + HALF[out]) + 1e-30)
 
 
+@pytest.mark.parametrize("T, k, E, N, K, slots", [
+    (1600, 1, 1, 2064, 544, False), (1590, 1, 1, 2048, 160, False), (4100, 1, 1, 2064, 288, False), (4097, 1, 1, 2048, 1280, False), (4096, 1, 1, 2064, 800, False),
+    (1000, 2, 3, 1600, 256, True), (1700, 4, 9, 1040, 1056, False), (2000, 3, 5, 2064, 96, True), (3000, 2, 2, 1536, 2304, False),
+])
+def test_mx_product_larger_tiles(ctx, T, k, E, N, K, slots):
+    """Enough rows for the tiles of 64 and of 128 slots; odd counts, and all lengths of a last stage (1 to 7 blocks, none)."""
+    rng = np.random.default_rng(T + K)
+    w, x = mx_random(rng, E, N, K), mx_random(rng, *((T, k, K) if slots else (T, K)))
+    idx = experts(rng, T, k, E, "any")
+    want = O.product(O.mx_values(*w), O.mx_values(*x), idx, False)
+    W, X, i = B.Mx(*map(dev, w)), B.Mx(*map(dev, x)), dev(idx) if E > 1 else None
+    assert np.array_equal(np64(B.smoe_mx_product(ctx, W, X, idx=i, out_dtype=torch.float32)), want)
+    assert torch.equal(B.smoe_mx_product(ctx, W, X, idx=i).cpu(), torch.from_numpy(want).float().bfloat16())
+    want = O.silu(want[..., 0::2]) * want[..., 1::2]
+    for out in ("f32", "bf16"):
+        got = B.smoe_mx_product(ctx, W, X, idx=i, swiglu=True, out_dtype=DT[out])
+        close(got, want, np.abs(want) * (8 * U32 + HALF[out]) + 1e-30)
+
+
 @pytest.mark.parametrize("T, k, E, N, K", [(100, 4, 16, 160, 2048), (40, 1, 1, 64, 10944), (2, 2, 300 // 2, 32, 65536)])
 def test_mx_product_of_quantised_numbers(ctx, T, k, E, N, K):
     rng = np.random.default_rng(K)

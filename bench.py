@@ -41,8 +41,10 @@ def main():
     ap.add_argument("--warmup", type=int, default=64)
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-steps", type=int, default=40)
-    ap.add_argument("--workload", choices=["decode", "prefill", "stack-qwen", "stack-dsv2"], default="decode",
-                    help="decode (default, the headline metric) or the prefill grouped GEMM of one Qwen-shaped layer")
+    ap.add_argument("--workload", choices=["decode", "prefill", "stack-qwen", "stack-dsv2", "mxfp4-block"], default="decode",
+                    help="decode (default, the headline metric); the prefill grouped GEMM of one Qwen-shaped layer; whole decode steps; or mxfp4-block: norm, "
+                         "score routing, experts in microscaled 4-bit floats and residual norm of one DeepSeek-V2-Lite-shaped layer (--tokens up to 16, or "
+                         "--prefill-tokens)")
     ap.add_argument("--group", type=int, default=0, choices=[0, 32, 64, 128],
                     help="decode: quantisation group of the expert weights (default: the workload's 128; 32 is the "
                          "paper's expert format, with four times the scales and zero-points)")
@@ -96,6 +98,8 @@ def main():
         return prefill_bench(args)
     if args.workload in ("stack-qwen", "stack-dsv2"):
         return stack_bench(args)
+    if args.workload == "mxfp4-block":
+        return mxfp4_block_bench(args)
     global PLANE_BITS
     bh, bl = {"84": (8, 4), "63": (6, 3), "42": (4, 2)}[args.nest]
     PLANE_BITS = bl
@@ -482,6 +486,66 @@ def prefill_bench(args):
     if not args.no_cpu_baseline and not args.with_shared:
         out["cpu_baseline"] = cpu_baseline_prefill(wl, T, min(args.cpu_steps, 16), idx_g.cpu().numpy(), w_g.cpu().numpy())
     print(json.dumps(out))
+
+
+def mxfp4_block_bench(args):
+    """One MoE block around MXFP4 experts (64 routed, d_model 2048, d_ff 1408, top-6): norm of the residual stream, sigmoid routing in 8
+    groups with a balance bias, gate/up product with SwiGLU, down product, and the residual norm that joins the slots.  --tokens (1 to 16) as
+    a decode step, --prefill-tokens as a prompt with quantised activations.  A step is one such block, replayed from a HIP graph."""
+    import torch
+    from paper_2512_12990_amd import binding as B, synth
+    wl = synth.DSV2_LAYER
+    E, d, f, k = wl.layer.n_experts, wl.layer.d_model, wl.layer.d_ff, wl.layer.top_k
+    T, few, dev = args.prefill_tokens or args.tokens, not args.prefill_tokens, "cuda:0"
+    s = torch.cuda.Stream()
+    ctx = B.Ctx(0, stream=s, workspace_bytes=0)
+    with torch.cuda.stream(s):
+        up, down = [], []
+        for e in range(E):
+            wg, wu, wd = synth.expert_weights(wl.seed, 0, e, d, f, "bf16", dev)
+            up.append(torch.stack([wg, wu], 1).reshape(2 * f, d))          # gate and up rows in turn
+            down.append(wd)
+        up, down = (B.smoe_mx_quantize(ctx, torch.stack(w)) for w in (up, down))
+        h = synth.activations(wl.seed, T, d, "f32").to(dev)
+        wr, bias = synth.router_weight(wl.seed, 0, E, d).to(dev), torch.zeros(E, device=dev)
+        one = torch.ones(d, dtype=torch.bfloat16, device=dev)
+
+        def step():
+            _, x = B.smoe_residual_norm(ctx, h, pre_w=one)
+            idx, w = B.smoe_route_scores(ctx, k, x=x, w_router=wr, score="sigmoid", n_group=8, topk_group=4, group_score="top2", bias=bias, norm_topk=True)
+            if few:
+                y = B.smoe_mx_matvec(ctx, down, B.smoe_mx_matvec(ctx, up, x, idx=idx, swiglu=True), idx=idx)
+            else:
+                mid = B.smoe_mx_product(ctx, up, B.smoe_mx_quantize(ctx, x), idx=idx, swiglu=True)
+                y = B.smoe_mx_product(ctx, down, B.smoe_mx_quantize(ctx, mid), idx=idx)
+            return B.smoe_residual_norm(ctx, h, y=y, slot_w=w, pre_w=one), idx
+
+        _, idx = step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    steps = min(args.steps, 1024 if few else 50)
+    ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    with torch.cuda.stream(s):
+        for _ in range(args.warmup):
+            graph.replay()
+        torch.cuda.synchronize()
+        ev0.record(s)
+        for _ in range(steps):
+            graph.replay()
+        ev1.record(s)
+    torch.cuda.synchronize()
+    us = ev0.elapsed_time(ev1) / steps * 1e3
+    used = int(torch.unique(idx).numel())
+    wbytes, flops = used * 3 * d * f * 17 / 32, 2.0 * T * k * 3 * d * f
+    print(json.dumps({
+        "metric": "MoE block us (%d tokens, norm + score routing + MXFP4 experts + residual norm)" % T, "value": us, "unit": "us/block", "n_gpus": 1, "steps": steps,
+        "warmup": args.warmup, "ms_per_step": us / 1e3, "higher_is_better": False, "scaling": "weak", "vs_baseline": None,
+        "dtype": "bf16 activations, MXFP4 weights" + ("" if few else " and products"), "data": "synthetic",
+        "config": {"workload": "DeepSeek-V2-Lite-shaped block, MXFP4 experts", "tokens": T, "n_experts": E, "top_k": k, "d_model": d, "d_ff": f, "experts_used": used},
+        "roofline": {"bound": "hbm", "achieved": wbytes / us / 1e3, "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": wbytes / us / 1e3 / HBM_PEAK_GBPS,
+                     "weight_bytes_per_step": wbytes, "flops_per_step": flops, "tflops": flops / us / 1e6}}))
 
 
 def stack_bench(args):

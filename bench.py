@@ -498,7 +498,7 @@ def mxfp4_block_bench(args):
     E, d, f, k = wl.layer.n_experts, wl.layer.d_model, wl.layer.d_ff, wl.layer.top_k
     T, few, dev = args.prefill_tokens or args.tokens, not args.prefill_tokens, "cuda:0"
     s = torch.cuda.Stream()
-    ctx = B.Ctx(0, stream=s, workspace_bytes=0)
+    ctx = B.Ctx(0, stream=s)
     with torch.cuda.stream(s):
         up, down = [], []
         for e in range(E):

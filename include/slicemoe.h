@@ -175,7 +175,8 @@ int smoe_route(smoe_ctx* ctx, int T, int E, int k, int d_model, const float* log
  * the expert's own (and with norm_topk those beside it).
  * E <= 256, k <= 16, n_group <= 64 and a divisor of E, k <= topk_group * E / n_group, T <= 2^22 (SMOE_ESHAPE).  With the
  * mat-vec the activations of a token stand in LDS: SMOE_ESIZE above 64 KiB (d_model about 28000 in bf16 and 14000 in fp32 less
- * what 12 E bytes take). */
+ * what 12 E bytes take); for one token a context with a workspace keeps the logits there and spreads the mat-vec over
+ * the device, with the same results. */
 enum { SMOE_SCORE_SOFTMAX = 0, SMOE_SCORE_SIGMOID = 1 };
 enum { SMOE_GROUP_MAX = 0, SMOE_GROUP_TOP2 = 1 };
 int smoe_route_scores(smoe_ctx* ctx, int T, int E, int k, int d_model, const float* logits_dev, const void* x_dev,
@@ -309,7 +310,7 @@ int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const uint8_t* code
  * Sums are fp32, y_dev is rounded once to out_dtype.  scratch_dev (smoe_mx_product_bytes; not used and may be NULL where
  * idx_dev is NULL) belongs to the call until its work is done: calls that may overlap need one each.
  * N a multiple of 16 up to 2^20, K of 32 up to 65536, N*K < 2^32, the rows of x less than 2^31 bytes of codes, E <= 256, k <= 16,
- * T*k <= 2^22, T*k*N <= 2^35 (SMOE_ESHAPE). */
+ * T*k <= 2^22, T*k*N <= 2^35 (SMOE_ESHAPE).  y_dev must not overlap what is read. */
 int smoe_mx_product_bytes(int T, int k, int E, size_t* scratch_bytes);
 int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
                     int k, const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, int x_slots, const int32_t* idx_dev,

@@ -145,6 +145,19 @@ def test_route_scores_from_activations(ctx, T, E, d, act):
     assert np.abs(got - best).max() <= 2 * off
 
 
+@pytest.mark.parametrize("E, d, act", [(64, 2048, "bf16"), (256, 520, "f32"), (7, 96, "bf16")])
+def test_route_scores_one_token_with_a_workspace(ctx, E, d, act):
+    """The mat-vec spread over the device, logits in the workspace: the bits of the call without one."""
+    g = torch.Generator().manual_seed(E)
+    c = B.Ctx(0)
+    for _ in range(3):
+        x, wr = torch.randn((1, d), generator=g).to(DT[act]).cuda(), (torch.randn((E, d), generator=g) * 0.05).cuda()
+        a = B.smoe_route_scores(c, 3, x=x, w_router=wr, score="sigmoid", norm_topk=True)
+        b = B.smoe_route_scores(ctx, 3, x=x, w_router=wr, score="sigmoid", norm_topk=True)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    c.close()
+
+
 # ------------------------------------------------------------------------------------ residual norm
 def check_norm(ctx, T, d, k, act="bf16", res="f32", post=False, gate=None, pre=True, slot_w=True, scale=1.0, eps=1e-6, with_res=True, with_y=True, x=True,
                in_place=False, data=None, seed=0):

@@ -150,8 +150,8 @@ __device__ __forceinline__ void select_scores_wave(const ScoreArgs& a, int t, co
 // of a softmax: argument 1, exponential 2, divisor and product 2) and the sum with a bias below 4 by one of its own: two keys more than
 // 2^-20 max(1, |key|) apart are in order.  Logits more than 2^-30 apart, and where they decide
 // sigmoids at most 15, have binary64 scores that differ (slope of the sigmoid at 15: 3e-7).
-//   Bound: vector issue, about 90 instructions a pick for the four tokens of a wave.  16384 tokens, 256 experts in 8 groups, top-8: 39 us with the long form alone,
-// 28 us with a short form of one token per wave.
+//   Bound: vector issue.  16384 tokens, 256 experts in 8 groups, top-8: 39 us with the long form alone, 28 with a short form of one token per wave, 22 with the pick
+// found by comparing and taken out by a mask (140 instructions a pick, now 50), 20 now, of which some 6 are the few tokens that need the long form.
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
 // the four steps of a reduction over a row of sixteen lanes: neighbour, neighbouring pair, other four of eight, other eight
 #define ROW_REDUCE(v, OP)      \
@@ -228,7 +228,7 @@ __device__ __forceinline__ bool select_scores_row(const ScoreArgs& a, int t, boo
   auto apart = [&](float hi, float lo) { return hi - lo > unit * (by_score ? fmaxf(1.0f, fabsf(hi)) : 1.0f); };
   uint32_t ord[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; j++) ord[j] = rl * NJ + j < E ? orderable(v[j]) : 0u;
+  for (int j = 0; j < NJ; j++) ord[j] = rl * NJ + j < E ? (orderable(v[j]) & ~15u) | (15u - j) : 0u;
   if (a.n_group > 1) {
     const int lpg = a.group_size / NJ;                                  // lanes of a group: a power of two up to 8
     float b0 = v[0], b1 = -INFINITY;
@@ -255,27 +255,24 @@ __device__ __forceinline__ bool select_scores_row(const ScoreArgs& a, int t, boo
 #pragma unroll
     for (int j = 0; j < NJ; j++) ord[j] = chosen ? ord[j] : 0u;
   }
-  // k picks and, where there is one, the best that is left
+  // k picks and, where there is one, the best that is left.  The lowest four bits of a key are the expert's place in its lane, so that a pick is a
+  // minimum of distances below the last one, without masks: keys not below it wrap round to more than any distance.
   int mysel = 0;
-  float last = 0.0f;
+  uint32_t top = 0;
   const int avail = a.topk_group * a.group_size;
   for (int r = 0; r <= k && r < avail; r++) {
-    uint32_t top = ord[0];
+    uint32_t mine = 0xFFFFFFFFu;
 #pragma unroll
-    for (int j = 1; j < NJ; j++) top = max(top, ord[j]);
-    top = row_umax(top);
-    const float vt = unorderable(top);
-    fine = fine && (r == 0 || apart(last, vt) || (!by_score && last == vt)) && (by_score || !sigmoid || vt <= 15.0f);
-    last = vt;
+    for (int j = 0; j < NJ; j++) mine = min(mine, top - 1u - ord[j]);
+    const uint32_t step = row_umin(mine), next = top - 1u - step;
+    // what the four bits hide is counted in: lower bound of the last key against upper bound of this one
+    const float vt = unorderable(next | 15u);
+    fine = fine && (r == 0 || apart(unorderable(top & ~15u), vt)) && (by_score || !sigmoid || vt <= 15.0f);
+    top = next;
     if (r == k) break;
-    uint32_t mine = 0xFFFFu;                                            // the lowest index among equal keys
-#pragma unroll
-    for (int j = NJ - 1; j >= 0; j--) mine = ord[j] == top ? (uint32_t)(rl * NJ + j) : mine;
-    const uint32_t e = row_umin(mine);
-    if (rl == r) mysel = (int)e;
-    const int at = (int)e - rl * NJ;
-#pragma unroll
-    for (int j = 0; j < NJ; j++) ord[j] = at == j ? 0u : ord[j];
+    const uint32_t who = (uint32_t)(__ballot(mine == step) >> (lane & 48)) & 0xFFFFu;      // (one lane: two with the same key are not apart, and show below)
+    fine = fine && !(who & (who - 1u));
+    if (rl == r) mysel = (int)(__builtin_ctz(who) * NJ + 15u - (top & 15u));
   }
   fine = !((__ballot(!fine) >> (lane & 48)) & 0xFFFFu);
   double w = 0.0;
@@ -376,7 +373,7 @@ extern "C" int smoe_route_scores(smoe_ctx* ctx, int T, int E, int k, int d_model
     return launch_scores_x<SMOE_BF16, 8>(ctx, a, T);
   }
   // The short form needs rows of 16-byte pieces and groups of whole lanes, a power of two of them up to 8.  With few tokens its longer chain of
-  // instructions counts and not their number: 2047 tokens, 60 experts, top-4 5.4 us, by the long form 3.8; 16384, 256 experts, top-8 23 and 39.
+  // instructions counts and not their number: 2047 tokens, 60 experts, top-4 5.4 us, by the long form 3.8; 16384, 256 experts, top-8 20 and 39.
   const size_t lds = n_group > 1 ? (size_t)SC_WAVES * E * 8 : 0;
   const int nj = E <= 64 ? 4 : E <= 128 ? 8 : 16, lpg = E / n_group / nj;
   const bool brief = T > 2048 && E % 4 == 0 && (n_group == 1 || (E / n_group % nj == 0 && (lpg & (lpg - 1)) == 0));

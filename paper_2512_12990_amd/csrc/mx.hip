@@ -93,7 +93,7 @@ extern "C" int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const ui
 // y[slot] = W[idx[slot]] x, W microscaled, x as it is.  Bound: the bytes of the selected matrices.
 //   A work-group takes 16 RT weight rows of one expert and up to 16 of the slots that chose this expert, so that every weight
 // byte is read once however many tokens share it.  Work-groups go by slots (that of a slot that is not the first of its expert has
-// nothing to do) or, with fewer experts than slots, by experts.  Its four waves share the columns out, 128 at a time (32 columns of a row are one 16-byte load of a lane), and add their
+// nothing to do) or, with fewer experts than slots, by experts.  Its four or eight waves share the columns out, 128 at a time (32 columns of a row are one 16-byte load of a lane), and add their
 // sums up through LDS.
 //   Codes are expanded to bf16, which holds e2m1 times a power of two exactly, and multiplied by matrix instructions with
 // fp32 sums.  fp32 activations go in as three bf16 numbers whose sum they are (8 + 8 + 8 bits, cut off, not rounded), so
@@ -103,7 +103,6 @@ struct MatvecArgs {
   int E, N, K, T, k, x_slots, swiglu, by_expert;
 };
 
-#define MV_WAVES 4
 template <int ACT> __device__ __forceinline__ void store1(void* p, size_t i, float v) {
   if (ACT == SMOE_F32) ((float*)p)[i] = v;
   else ((__bf16*)p)[i] = (__bf16)v;
@@ -138,7 +137,7 @@ __device__ __forceinline__ void operands(const RawX<ACT>& r, bool ok, bf16x8 (&p
   }
 }
 
-template <int ACT, int RT, int U>      // U: units of 128 columns in flight
+template <int ACT, int RT, int MV_WAVES>
 __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) {
   constexpr int PARTS = ACT == SMOE_F32 ? 3 : 1, ROWS = 16 * RT;
   __shared__ int slots[SMOE_MAX_MULTI * SMOE_MAX_TOPK];
@@ -185,46 +184,39 @@ __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) 
     f32x4 acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; t++) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int u0 = wave * per; u0 < u_end; u0 += U) {
-      u32x4 w[U][RT];
-      uint32_t sb[U][RT];
-      RawX<ACT> x[U][4];
+    for (int u = wave * per; u < u_end; u++) {
+      const int bc = min(u * 4 + g, nb - 1);
+      u32x4 w[RT];
+      uint32_t sb[RT];
+      RawX<ACT> x[4];
 #pragma unroll
-      for (int u = 0; u < U; u++) {
-        const int bc = min((u0 + u) * 4 + g, nb - 1);
-#pragma unroll
-        for (int t = 0; t < RT; t++) {
-          w[u][t] = *(const u32x4*)(wc[t] + (size_t)bc * 16);
-          sb[u][t] = ws[t][bc];
-        }
-#pragma unroll
-        for (int s = 0; s < 4; s++)
-#pragma unroll
-          for (int v = 0; v < (ACT == SMOE_F32 ? 2 : 1); v++)
-            x[u][s].v[v] = *(const u32x4*)((const uint8_t*)a.x + (xrow + (size_t)bc * 32 + s * 8) * (ACT == SMOE_F32 ? 4 : 2) + v * 16);
+      for (int t = 0; t < RT; t++) {
+        w[t] = *(const u32x4*)(wc[t] + (size_t)bc * 16);
+        sb[t] = ws[t][bc];
       }
 #pragma unroll
-      for (int u = 0; u < U; u++) {
-        // a block that does not exist: activations and codes 0
-        const bool ok = u0 + u < u_end && (u0 + u) * 4 + g < nb;
-        float sc[RT];
+      for (int s = 0; s < 4; s++)
 #pragma unroll
-        for (int t = 0; t < RT; t++) sc[t] = ok ? mx_scale(sb[u][t]) : 1.0f;
+        for (int v = 0; v < (ACT == SMOE_F32 ? 2 : 1); v++)
+          x[s].v[v] = *(const u32x4*)((const uint8_t*)a.x + (xrow + (size_t)bc * 32 + s * 8) * (ACT == SMOE_F32 ? 4 : 2) + v * 16);
+      const bool ok = u * 4 + g < nb;                         // a block that does not exist: activations 0, scale 1
+      float sc[RT];
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
-          bf16x8 p[PARTS];
-          operands<ACT>(x[u][s], ok, p);
+      for (int t = 0; t < RT; t++) sc[t] = ok ? mx_scale(sb[t]) : 1.0f;
 #pragma unroll
-          for (int t = 0; t < RT; t++) {
-            const uint32_t q = w[u][t][s];
-            union { bf16x2 h[4]; bf16x8 v; } wf;
-            wf.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 0);
-            wf.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 1);
-            wf.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 2);
-            wf.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 3);
+      for (int s = 0; s < 4; s++) {
+        bf16x8 p[PARTS];
+        operands<ACT>(x[s], ok, p);
 #pragma unroll
-            for (int m = PARTS - 1; m >= 0; m--) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, p[m], acc[t], 0, 0, 0);
-          }
+        for (int t = 0; t < RT; t++) {
+          const uint32_t q = w[t][s];
+          union { bf16x2 h[4]; bf16x8 v; } wf;
+          wf.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 0);
+          wf.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 1);
+          wf.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 2);
+          wf.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, sc[t], 3);
+#pragma unroll
+          for (int m = PARTS - 1; m >= 0; m--) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf.v, p[m], acc[t], 0, 0, 0);
         }
       }
     }
@@ -253,9 +245,9 @@ __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) 
   }
 }
 
-template <int ACT, int RT, int U> static void launch_matvec(smoe_ctx* ctx, const MatvecArgs& a) {
+template <int ACT, int RT, int MV_WAVES> static void launch_matvec(smoe_ctx* ctx, const MatvecArgs& a) {
   const dim3 grid((a.N + 16 * RT - 1) / (16 * RT), !a.idx ? 1 : a.by_expert ? a.E : a.T * a.k);
-  mx_matvec_kernel<ACT, RT, U><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
+  mx_matvec_kernel<ACT, RT, MV_WAVES><<<grid, 64 * MV_WAVES, 0, ctx->stream>>>(a);
 }
 
 extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T, int k,
@@ -269,18 +261,17 @@ extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t*
   if (!aligned16(w_codes_dev) || !aligned16(w_scales_dev) || !aligned16(x_dev) || !aligned16(idx_dev) || !aligned16(y_dev)) return SMOE_EALIGN;
   ON_DEVICE_OF(ctx);
   const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu, T > 1 && E < T * k};
-  // Rows of a work-group.  Four tiles share one fetch and one splitting of the activations, with one unit of columns in flight, so that many work-groups fit
-  // a CU; where that leaves too few work-groups, one tile and two units.  16 tokens, top-6 of 64, N 2048, K 1408, fp32: 32 us with four tiles, 73 with one;
-  // one token, N 8192, K 8192, bf16: 19.4 us with four (128 work-groups), 13.3 with one; one token, top-6, N 2816, K 2048, bf16 (264): 11.6 and 10.2; four
-  // tokens, top-4 of 60, the same matrices (704): 17.3 and 17.7; fp32, one token, top-6, N 2048, K 1408 (192): 8.2 and 10.8; 16 tokens,
-  // N 21888, K 2048, bf16 (342): 14.8 and 19.2.
+  // Rows of a work-group.  Four tiles share one fetch and one splitting of the activations between four waves, one unit of columns in flight each, so that many
+  // work-groups fit a CU; where that leaves too few work-groups, one tile and eight waves.  Microseconds with four tiles / with one: 16 tokens, top-6 of 64, N 2048,
+  // K 1408, fp32 30 / 62; 16 tokens, N 21888, K 2048, bf16 (342 work-groups) 15.0 / 18.9; 4 tokens, top-4 of 60, N 2816, K 2048 (704) 17.6 / 20.0; one token, top-6, the
+  // same matrices (264) 11.8 / 9.8; one token, dense, N 8192, K 8192 (128) 19.5 / 14.4, N 2048, K 10944 (32) 21.9 / 8.0; fp32, one token, top-6, N 2048, K 1408 (192) 8.4 / 8.7.
   const long long wgs = (long long)((N + 63) / 64) * (!idx_dev ? 1 : T * k < E ? T * k : E);
   if (act_dtype == SMOE_F32) {
-    if (wgs < 128) launch_matvec<SMOE_F32, 1, 2>(ctx, a);
-    else launch_matvec<SMOE_F32, 4, 1>(ctx, a);
+    if (wgs < 128) launch_matvec<SMOE_F32, 1, 8>(ctx, a);
+    else launch_matvec<SMOE_F32, 4, 4>(ctx, a);
   } else {
-    if (wgs < (T > 4 ? 256 : 512)) launch_matvec<SMOE_BF16, 1, 2>(ctx, a);
-    else launch_matvec<SMOE_BF16, 4, 1>(ctx, a);
+    if (wgs < (T > 4 ? 256 : 512)) launch_matvec<SMOE_BF16, 1, 8>(ctx, a);
+    else launch_matvec<SMOE_BF16, 4, 4>(ctx, a);
   }
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;

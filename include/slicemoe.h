@@ -307,11 +307,11 @@ int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const uint8_t* code
  * W [E,N,K]; idx_dev int32 [T,k] as a router leaves it (the same expert may occur twice; an index outside [0, E)
  * counts as the nearest expert), or NULL with E = 1 and k = 1: a plain product.  swiglu = 0: y_dev [T,k,N];
  * swiglu = 1: rows 2i and 2i+1 of W are the gate and the up row of column i and y_dev [T,k,N/2] is silu(gate) * up.
- * Sums are fp32, y_dev is rounded once to out_dtype.  scratch_dev (smoe_mx_product_bytes; not used and may be NULL where
- * idx_dev is NULL) belongs to the call until its work is done: calls that may overlap need one each.
+ * Sums are fp32, y_dev is rounded once to out_dtype.  scratch_dev (smoe_mx_product_bytes; may be NULL where that is 0, as for few
+ * slots, or idx_dev is NULL) belongs to the call until its work is done: calls that may overlap need one each.
  * N a multiple of 16 up to 2^20, K of 32 up to 65536, N*K < 2^32, the rows of x less than 2^31 bytes of codes, E <= 256, k <= 16,
  * T*k <= 2^22, T*k*N <= 2^35 (SMOE_ESHAPE).  y_dev must not overlap what is read. */
-int smoe_mx_product_bytes(int T, int k, int E, size_t* scratch_bytes);
+int smoe_mx_product_bytes(int T, int k, int E, int N, size_t* scratch_bytes);
 int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
                     int k, const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, int x_slots, const int32_t* idx_dev,
                     int swiglu, int out_dtype, void* scratch_dev, size_t scratch_bytes, void* y_dev);

@@ -74,7 +74,7 @@ _SIGNATURES = {
     "smoe_residual_norm": "piiippppifppfiipp",
     "smoe_mx_quantize": "plipipp",
     "smoe_mx_dequantize": "plipppi",
-    "smoe_mx_product_bytes": "iiip",
+    "smoe_mx_product_bytes": "iiiip",
     "smoe_mx_product": "piiippiippipiipzp",
     "smoe_mx_matvec": "piiippiipiipip",
 }
@@ -512,9 +512,9 @@ def smoe_mx_dequantize(ctx: Ctx, m: Mx, dtype: torch.dtype = torch.float32) -> t
 
 
 @functools.lru_cache(maxsize=4096)
-def smoe_mx_product_bytes(T: int, k: int, E: int) -> int:
+def smoe_mx_product_bytes(T: int, k: int, E: int, N: int) -> int:
     n = C.c_size_t()
-    _chk(lib().smoe_mx_product_bytes(T, k, E, C.byref(n)), "smoe_mx_product_bytes")
+    _chk(lib().smoe_mx_product_bytes(T, k, E, N, C.byref(n)), "smoe_mx_product_bytes")
     return n.value
 
 
@@ -548,9 +548,10 @@ def smoe_mx_product(ctx: Ctx, w: Mx, x: Mx, idx: Optional[torch.Tensor] = None, 
     if scratch is not None:
         sp, size = _t(ctx, "scratch", scratch, _U8), scratch.numel()
     elif ip is not None and T:
-        size = smoe_mx_product_bytes(T, k, E)
-        scratch = x[0].new_empty(size)
-        sp = scratch.data_ptr()
+        size = smoe_mx_product_bytes(T, k, E, N)
+        if size:
+            scratch = x[0].new_empty(size)
+            sp = scratch.data_ptr()
     if y is None:
         y = x[0].new_empty(shape, dtype=out_dtype)
         yp = y.data_ptr()

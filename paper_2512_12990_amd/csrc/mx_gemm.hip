@@ -1,7 +1,7 @@
 // smoe_mx_product: Y[slot] = W[idx[slot]] X[token of slot], both operands microscaled 4-bit floats, by the scaled matrix
 // instructions (32 x 32 x 64, one e8m0 byte per 32 columns of a row, fp32 sums).
-//   group    one work-group per expert: the expert's slots, in order, and its tiles of at most BT of them
-//   gemm     a work-group per tile of slots and BN weight rows
+//   gemm     a work-group per tile of up to BT slots of one expert and BN weight rows; with few slots each finds its own among them
+//   group    before it, with many slots: one work-group per expert lists the expert's slots, in order, and its tiles
 #include "mx.hpp"
 #include <type_traits>
 
@@ -19,42 +19,52 @@ struct MxGemmArgs {
   const int32_t* rows;        // slots, BT for every tile (behind a tile's last slot that slot again), or null: slot i is row i
   const MxTile* tiles;        // null without rows
   const int* n_tiles;
+  const int32_t* idx;         // the slots' experts where the work-groups find their slots themselves, else null
   void* y;
-  int N, K, n, k, x_slots, x_rows, swiglu, out_f32, col_tiles, super;
+  int E, N, K, n, k, x_slots, x_rows, swiglu, out_f32, col_tiles, super;
 };
 
+// Experts of the slots i .. i + 15 of a run that ends at i1 (i a multiple of four), all loads in flight at once; -1 behind the run.  An index outside the experts
+// counts as the nearest of them.
+#define MG_RUN 16
+__device__ __forceinline__ void fetch_experts(const int32_t* idx, int i, int i1, int E, int (&v)[MG_RUN]) {
+  int4 q[MG_RUN / 4];
+#pragma unroll
+  for (int u = 0; u < MG_RUN; u += 4) {
+    q[u / 4] = make_int4(0, 0, 0, 0);
+    if (i + u + 4 <= i1) q[u / 4] = *(const int4*)(idx + i + u);
+    else {
+      if (i + u < i1) q[u / 4].x = idx[i + u];
+      if (i + u + 1 < i1) q[u / 4].y = idx[i + u + 1];
+      if (i + u + 2 < i1) q[u / 4].z = idx[i + u + 2];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < MG_RUN; u++) {
+    const int w = u % 4 == 0 ? q[u / 4].x : u % 4 == 1 ? q[u / 4].y : u % 4 == 2 ? q[u / 4].z : q[u / 4].w;
+    v[u] = i + u < i1 ? max(0, min(w, E - 1)) : -1;
+  }
+}
+__device__ __forceinline__ int wave_prefix(int v, int lane) {            // inclusive
+  for (int s = 1; s < 64; s <<= 1) { const int o = __shfl_up(v, s); if (lane >= s) v += o; }
+  return v;
+}
+
 // Work-group e: the slots of expert e, in order, to its tiles of bt.  Every work-group counts all slots, so that none waits
-// for another.  An index outside the experts counts as the nearest of them.
+// for another.
 //   Bound: one memory round trip and the launch; a thread's slots are fetched sixteen at a time before the first is used (one after the other: 9.9 us for
 // 8192 slots, 60 experts).
 __global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx, int n, int E, int bt, int32_t* rows, MxTile* tiles, int* n_tiles) {
   __shared__ int count[SMOE_MAX_EXPERTS];
   __shared__ int wtot[MG_THREADS / 64];
   __shared__ int last;
-  constexpr int RUN = 16;
+  constexpr int RUN = MG_RUN;
   const int e = (int)blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (tid < SMOE_MAX_EXPERTS) count[tid] = 0;
   // every thread owns a contiguous run of slots, a multiple of four
   const int c = ((n + MG_THREADS - 1) / MG_THREADS + 3) & ~3, i0 = min(n, tid * c), i1 = min(n, i0 + c);
   int v[RUN];
-  auto fetch = [&](int i) {                                             // experts of slots i .. i + 15 (-1 behind the run)
-    int4 q[RUN / 4];
-#pragma unroll
-    for (int u = 0; u < RUN; u += 4) {
-      q[u / 4] = make_int4(0, 0, 0, 0);
-      if (i + u + 4 <= i1) q[u / 4] = *(const int4*)(idx + i + u);
-      else {
-        if (i + u < i1) q[u / 4].x = idx[i + u];
-        if (i + u + 1 < i1) q[u / 4].y = idx[i + u + 1];
-        if (i + u + 2 < i1) q[u / 4].z = idx[i + u + 2];
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < RUN; u++) {
-      const int w = u % 4 == 0 ? q[u / 4].x : u % 4 == 1 ? q[u / 4].y : u % 4 == 2 ? q[u / 4].z : q[u / 4].w;
-      v[u] = i + u < i1 ? max(0, min(w, E - 1)) : -1;
-    }
-  };
+  auto fetch = [&](int i) { fetch_experts(idx, i, i1, E, v); };
   fetch(i0);
   __syncthreads();
   int mine = 0;
@@ -64,8 +74,7 @@ __global__ __launch_bounds__(MG_THREADS) void mx_group_kernel(const int32_t* idx
     for (int u = 0; u < RUN; u++)
       if (v[u] >= 0) { mine += v[u] == e; atomicAdd(&count[v[u]], 1); }
   }
-  int incl = mine;
-  for (int s = 1; s < 64; s <<= 1) { const int o = __shfl_up(incl, s); if (lane >= s) incl += o; }
+  const int incl = wave_prefix(mine, lane);
   if (lane == 63) wtot[wave] = incl;
   __syncthreads();
   int t0 = 0;                                                           // tiles of the experts before e
@@ -136,32 +145,88 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   constexpr uint32_t NONE = 0x80000000u;                               // beyond every buffer: nothing is fetched
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
+  int* slots = (int*)(As + S::slots_at(UNAL));                          // the tile's slots
+  // ---- how many tiles there are.  With a.idx: count the experts' slots and number their tiles (lane l: experts l, l + 64, ...)
+  int *count = (int*)As, *wtot = count + SMOE_MAX_EXPERTS;             // (where the codes will be)
+  const int run_len = ((a.n + 64 * NW - 1) / (64 * NW) + 3) & ~3, i0 = min(a.n, tid * run_len), i1 = min(a.n, i0 + run_len);
+  int v[MG_RUN], cnt[SMOE_MAX_EXPERTS / 64], first[SMOE_MAX_EXPERTS / 64];
+  int n_tiles = 0;
+  if (a.idx) {
+    fetch_experts(a.idx, i0, i1, a.E, v);
+    for (int i = tid; i < SMOE_MAX_EXPERTS; i += 64 * NW) count[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < MG_RUN; u++)
+      if (v[u] >= 0) atomicAdd(&count[v[u]], 1);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < SMOE_MAX_EXPERTS / 64; q++) {
+      const int x = lane + 64 * q;
+      cnt[q] = count[x];
+      first[q] = 0x7FFFFFFF;
+      if (64 * q < a.E) {                                              // (uniform)
+        const int t = (cnt[q] + BT - 1) / BT, sum = wave_prefix(t, lane);
+        if (x < a.E) first[q] = n_tiles + sum - t;
+        n_tiles += __builtin_amdgcn_readlane(sum, 63);
+      }
+    }
+  } else {
+    n_tiles = a.rows ? uni(*a.n_tiles) : (a.n + BT - 1) / BT;
+  }
   // ---- which tile.  Consecutive items, `super` tiles of slots side by side for every tile of weight rows, stay on one XCD, whose L2 then serves the rows
   // they share
-  const int n_tiles = a.rows ? uni(*a.n_tiles) : (a.n + BT - 1) / BT;
   const int n_items = n_tiles * a.col_tiles, run = (n_items + 7) >> 3;
   const int place = (int)blockIdx.x >> 3, item = ((int)blockIdx.x & 7) * run + place;
   if (place >= run || item >= n_items) return;
   const int per_band = a.super * a.col_tiles, band = uni(item / per_band), in_band = item - band * per_band;
   const int band_n = min(a.super, n_tiles - band * a.super), ct = uni(in_band / band_n), ti = band * a.super + in_band - ct * band_n;
   MxTile tile;
-  if (a.rows) {
-    tile = a.tiles[ti];
-    tile.expert = uni(tile.expert); tile.count = uni(tile.count);
+  if (a.idx) {
+    // the last expert whose first tile is not past ti, and the slots of its rows m0 .. on
+    int e = -1, m0 = 0, of = 0;
+#pragma unroll
+    for (int q = 0; q < SMOE_MAX_EXPERTS / 64; q++) e += (int)__builtin_popcountll(__ballot(first[q] <= ti));
+    e = uni(e);
+#pragma unroll
+    for (int q = 0; q < SMOE_MAX_EXPERTS / 64; q++)
+      if (q == e >> 6) {
+        m0 = (ti - __builtin_amdgcn_readlane(first[q], e & 63)) * BT;
+        of = __builtin_amdgcn_readlane(cnt[q], e & 63);
+      }
+    tile = MxTile{e, min(BT, of - m0)};
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < MG_RUN; u++) mine += v[u] == e;
+    const int incl = wave_prefix(mine, lane);
+    if (lane == 63) wtot[wave] = incl;
+    __syncthreads();
+    int p = incl - mine - m0;
+#pragma unroll
+    for (int w = 0; w < NW; w++) p += w < wave ? wtot[w] : 0;
+#pragma unroll
+    for (int u = 0; u < MG_RUN; u++)
+      if (v[u] == e) {
+        if (p >= 0 && p < BT) slots[p] = i0 + u;
+        p++;
+      }
+    __syncthreads();
   } else {
-    tile = MxTile{0, min(BT, a.n - ti * BT)};
+    tile = a.rows ? a.tiles[ti] : MxTile{0, min(BT, a.n - ti * BT)};
+    tile.expert = uni(tile.expert); tile.count = uni(tile.count);
+    if (tid < BT) slots[tid] = a.rows ? a.rows[(size_t)ti * BT + tid] : ti * BT + min(tid, tile.count - 1);
   }
-  const int32_t* tile_rows = a.rows + (size_t)ti * BT;
   const int nb = a.K >> 5, n0 = ct * BN, n_st = (nb + 7) >> 3, n_full = nb >> 3;
   const uint32_t rowb = (uint32_t)(a.K >> 1);
   const u32x4 rwc = buffer_of(a.wc + (size_t)tile.expert * a.N * rowb, (uint32_t)a.N * rowb);
   const u32x4 rws = buffer_of(a.ws + (size_t)tile.expert * a.N * nb, (uint32_t)a.N * (uint32_t)nb);
   const u32x4 rxc = buffer_of(a.xc, (uint32_t)a.x_rows * rowb);
   const u32x4 rxs = buffer_of(a.xs, ((uint32_t)a.x_rows * (uint32_t)nb + 3u) & ~3u);      // (whole dwords: every one fetched holds a byte of the array)
-  auto slot_of = [&](int r) { return a.rows ? tile_rows[r] : ti * BT + min(r, tile.count - 1); };
-  auto x_row = [&](int r) { const int slot = slot_of(r); return (uint32_t)(a.x_slots ? slot : slot / a.k); };      // row of X of the tile's slot r
-  int* slots = (int*)(As + S::slots_at(UNAL));                          // for the result
-  if (tid < BT) slots[tid] = slot_of(tid);
+  // row of X of the tile's slot r; behind the last slot that slot again
+  auto x_row = [&](int r) {
+    const int rc = min(r, tile.count - 1);
+    const int slot = a.idx ? slots[rc] : a.rows ? a.rows[(size_t)ti * BT + rc] : ti * BT + rc;
+    return (uint32_t)(a.x_slots ? slot : slot / a.k);
+  };
   // ---- addresses.  Code load q of a wave: rows 8 (NW q + wave) .. + 7 of the weight rows, then of the token rows; a lane's piece is the same for all q
   const int pr = lane >> 3, piece = (lane & 7) ^ (((8 * wave + pr) >> 1) & 7);
   const uint32_t wv = (uint32_t)(n0 + 8 * wave + pr) * rowb + piece * 16u;
@@ -380,12 +445,12 @@ static const MxShape g_shapes[3] = {{32, 128, 2, 1.0}, {64, 128, 2, 1.34}, {128,
 static long long likely_tiles(int n, int E, int bt) { return E == 1 ? (n + bt - 1) / bt : n / bt + (n < E ? n : E + 1) / 2; }
 // The shape with the least rounds of work-groups times their cost; one round at least.  Microseconds of shapes 0 / 1 / 2 (top-6 of 64, N 2816, K 2048): 100
 // tokens 39.0 / 39.3 / 45.3, 300 47.2 / 44.4 / 53.1, 800 75.8 / 61.9 / 66.6, 1500 118 / 87.7 / 82.2; dense, N 2048, K 2048: 256 rows 6.1 / 7.5 / 11.7, 4096 28.2 / 21.0 / 16.9.
-static int pick_shape(int n, int E, int N, int n_cu) {
+static double rounds_of(const MxShape& s, int n, int E, int N) { return (double)likely_tiles(n, E, s.bt) * ((N + s.bn - 1) / s.bn) / (256.0 * s.per_cu); }      // (256 CUs)
+static int pick_shape(int n, int E, int N) {
   int best = 0;
   double least = 0.0;
   for (int i = 0; i < 3; i++) {
-    const MxShape& s = g_shapes[i];
-    const double rounds = (double)likely_tiles(n, E, s.bt) * ((N + s.bn - 1) / s.bn) / ((double)s.per_cu * n_cu), t = (rounds > 1.0 ? rounds : 1.0) * s.cost;
+    const double rounds = rounds_of(g_shapes[i], n, E, N), t = (rounds > 1.0 ? rounds : 1.0) * g_shapes[i].cost;
     if (i == 0 || t < least) { best = i; least = t; }
   }
   return best;
@@ -432,10 +497,19 @@ static int check_product(int E, int T, int k) {
   return SMOE_OK;
 }
 
-extern "C" int smoe_mx_product_bytes(int T, int k, int E, size_t* scratch_bytes) {
+// Whether work-groups find their slots themselves: at most sixteen for a thread to look through, and at most two rounds of work-groups, each of which pays for
+// the search what the list would cost all of them once and a launch.  Microseconds without / with a list (top-6 of 64, N 2816, K 2048): 32 tokens (1.6 rounds) 30.0 / 30.9, 100
+// tokens (2.2) 41.0 / 39.0, 512 tokens (4.6) 56.3 / 53.5; 500 tokens, top-2 of 8, N 512, K 1024 (0.3) 7.3 / 9.7.
+static bool searches_itself(int n, int E, int N, int shape) {
+  const int waves[3] = {MgShape<1, 4, 1, 1>::NW, MgShape<2, 2, 1, 2>::NW, MgShape<2, 4, 2, 2>::NW};
+  return n <= MG_RUN * 64 * waves[shape] && rounds_of(g_shapes[shape], n, E, N) <= 2.0;
+}
+
+extern "C" int smoe_mx_product_bytes(int T, int k, int E, int N, size_t* scratch_bytes) {
   if (!scratch_bytes) return SMOE_EINVAL;
   if (const int rc = check_product(E, T, k)) return rc;
-  *scratch_bytes = product_layout(T, k, E).total;
+  if (const int rc = check_mx_matrix(N, 32)) return rc;
+  *scratch_bytes = T == 0 || searches_itself(T * k, E, N, pick_shape(T * k, E, N)) ? 0 : product_layout(T, k, E).total;
   return SMOE_OK;
 }
 
@@ -447,30 +521,34 @@ extern "C" int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t
   if (const int rc = check_mx_matrix(N, K)) return rc;
   if (T == 0) return SMOE_OK;
   if ((long long)T * (x_slots ? k : 1) * (K / 2) >= (1ll << 31) || (long long)T * k * N > (1ll << 35) || (!idx_dev && (E != 1 || k != 1))) return SMOE_ESHAPE;
-  if (!w_codes_dev || !w_scales_dev || !x_codes_dev || !x_scales_dev || !y_dev || (idx_dev && !scratch_dev)) return SMOE_EINVAL;
+  const int n = T * k, shape = pick_shape(n, E, N);
+  const bool lists = idx_dev && !searches_itself(n, E, N, shape);
+  if (!w_codes_dev || !w_scales_dev || !x_codes_dev || !x_scales_dev || !y_dev || (lists && !scratch_dev)) return SMOE_EINVAL;
   if (!aligned16(w_codes_dev) || !aligned16(w_scales_dev) || !aligned16(x_codes_dev) || !aligned16(x_scales_dev) || !aligned16(idx_dev) ||
       !aligned16(y_dev) || !aligned16(scratch_dev))
     return SMOE_EALIGN;
   const MxProductLayout l = product_layout(T, k, E);
-  if (idx_dev && scratch_bytes < l.total) return SMOE_ESIZE;
+  if (lists && scratch_bytes < l.total) return SMOE_ESIZE;
   ON_DEVICE_OF(ctx);
-  const int n = T * k;
   uint8_t* s = (uint8_t*)scratch_dev;
-  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, y_dev, N, K, n, k, x_slots, T * (x_slots ? k : 1),
+  MxGemmArgs a{w_codes_dev, w_scales_dev, x_codes_dev, x_scales_dev, nullptr, nullptr, nullptr, nullptr, y_dev, E, N, K, n, k, x_slots, T * (x_slots ? k : 1),
                swiglu, out_dtype == SMOE_F32, 0, 1};
-  const int shape = pick_shape(n, E, N, ctx->n_cu);
   const int bt = g_shapes[shape].bt;
   a.col_tiles = (N + g_shapes[shape].bn - 1) / g_shapes[shape].bn;
   int max_tiles = (n + bt - 1) / bt;
   a.super = max_tiles / E < 1 ? 1 : max_tiles / E > 8 ? 8 : max_tiles / E;
   if (idx_dev) {
-    int32_t* rows = (int32_t*)(s + l.rows);
-    MxTile* tiles = (MxTile*)(s + l.tiles);
-    int* n_tiles = (int*)(s + l.n_tiles);
     max_tiles = max_tiles_of(n, E, bt);
-    mx_group_kernel<<<E, MG_THREADS, 0, ctx->stream>>>(idx_dev, n, E, bt, rows, tiles, n_tiles);
-    HIPCHK(ctx, hipGetLastError());
-    a.rows = rows; a.tiles = tiles; a.n_tiles = n_tiles;
+    if (!lists) {
+      a.idx = idx_dev;
+    } else {
+      int32_t* rows = (int32_t*)(s + l.rows);
+      MxTile* tiles = (MxTile*)(s + l.tiles);
+      int* n_tiles = (int*)(s + l.n_tiles);
+      mx_group_kernel<<<E, MG_THREADS, 0, ctx->stream>>>(idx_dev, n, E, bt, rows, tiles, n_tiles);
+      HIPCHK(ctx, hipGetLastError());
+      a.rows = rows; a.tiles = tiles; a.n_tiles = n_tiles;
+    }
   }
   const unsigned grid = ((unsigned)max_tiles * (unsigned)a.col_tiles + 7) / 8 * 8;
   if (shape == 0) return launch_gemm<1, 4, 1, 1>(ctx, a, grid, 0);

@@ -131,7 +131,7 @@ def test_mx_quantize_refuses(ctx, kw, rc):
 
 
 def _product(ctx, **kw):
-    a = dict(E=4, N=64, K=64, wc=P, ws=P, T=5, k=2, x=P, xs=P, slots=0, idx=P, sg=0, dt=0, scratch=P, nbytes=1 << 20, y=P)
+    a = dict(E=4, N=64, K=64, wc=P, ws=P, T=3000, k=2, x=P, xs=P, slots=0, idx=P, sg=0, dt=0, scratch=P, nbytes=1 << 20, y=P)
     a.update(kw)
     return B.lib().smoe_mx_product(ctx, *a.values())
 
@@ -152,12 +152,14 @@ def test_mx_product_refuses(ctx, kw, rc):
 def test_mx_product_bytes():
     n = C.c_size_t()
     lib = B.lib()
-    assert lib.smoe_mx_product_bytes(5, 2, 4, None) == -1
-    for args in [(-1, 2, 4), (5, 0, 4), (5, 17, 4), (5, 2, 0), (5, 2, 257), (1 << 22, 2, 4)]:
+    assert lib.smoe_mx_product_bytes(5, 2, 4, 64, None) == -1
+    for args in [(-1, 2, 4, 64), (5, 0, 4, 64), (5, 17, 4, 64), (5, 2, 0, 64), (5, 2, 257, 64), (1 << 22, 2, 4, 64), (5, 2, 4, 0), (5, 2, 4, 24)]:
         assert lib.smoe_mx_product_bytes(*args, C.byref(n)) == -2
-    # the sorted slots and, for each, room in the list of tiles
-    assert B.smoe_mx_product_bytes(2048, 4, 60) >= 2048 * 4 * 4
-    assert B.smoe_mx_product_bytes(0, 4, 60) >= 0
+    # the slots listed by expert and, for each tile, a record; none where there are few
+    assert B.smoe_mx_product_bytes(2048, 4, 60, 2816) >= 2048 * 4 * 4
+    assert B.smoe_mx_product_bytes(3000, 2, 4, 64) >= 6000 * 4
+    assert B.smoe_mx_product_bytes(0, 4, 60, 64) == 0 and B.smoe_mx_product_bytes(1024, 4, 60, 64) == 0
+    assert B.smoe_mx_product_bytes(1025, 4, 60, 64) > 0
 
 
 def _matvec(ctx, **kw):

@@ -332,9 +332,11 @@ def test_mx_product_exact(ctx, T, k, E, N, K, how, slots):
 @pytest.mark.parametrize("T, k, E, N, K, slots", [
     (1600, 1, 1, 2064, 544, False), (1590, 1, 1, 2048, 160, False), (4100, 1, 1, 2064, 288, False), (4097, 1, 1, 2048, 1280, False), (4096, 1, 1, 2064, 800, False),
     (1000, 2, 3, 1600, 256, True), (1700, 4, 9, 1040, 1056, False), (2000, 3, 5, 2064, 96, True), (3000, 2, 2, 1536, 2304, False),
+    (5000, 4, 7, 48, 96, False), (4600, 2, 3, 2064, 160, True), (1024, 4, 250, 32, 64, False), (1025, 4, 250, 32, 64, False), (4096, 1, 2, 32, 64, False), (8192, 1, 3, 2048, 64, False),
 ])
 def test_mx_product_larger_tiles(ctx, T, k, E, N, K, slots):
-    """Enough rows for the tiles of 64 and of 128 slots; odd counts, and all lengths of a last stage (1 to 7 blocks, none)."""
+    """Enough rows for the tiles of 64 and of 128 slots; odd counts, and all lengths of a last stage (1 to 7 blocks, none); slots that work-groups find
+    themselves (up to 4096 or 8192) and slots listed before."""
     rng = np.random.default_rng(T + K)
     w, x = mx_random(rng, E, N, K), mx_random(rng, *((T, k, K) if slots else (T, K)))
     idx = experts(rng, T, k, E, "any")
@@ -389,20 +391,20 @@ def test_mx_product_scales(ctx):
 
 def test_mx_product_buffers_and_scratch(ctx):
     rng = np.random.default_rng(9)
-    w, x = mx_random(rng, 6, 64, 128), mx_random(rng, 50, 128)
-    idx = experts(rng, 50, 3, 6, "any")
+    w, x = mx_random(rng, 6, 64, 128), mx_random(rng, 2100, 128)
+    idx = experts(rng, 2100, 3, 6, "any")
     W, X, i = B.Mx(*map(dev, w)), B.Mx(*map(dev, x)), dev(idx)
     want = B.smoe_mx_product(ctx, W, X, idx=i)
-    scratch = torch.full((B.smoe_mx_product_bytes(50, 3, 6),), 255, dtype=torch.uint8, device="cuda")
-    wide = torch.full((52, 3, 64), 7.0, dtype=torch.bfloat16, device="cuda")
-    got = B.smoe_mx_product(ctx, W, X, idx=i, scratch=scratch, y=wide[1:51])
-    assert got.data_ptr() == wide[1:51].data_ptr() and torch.equal(got, want)
-    assert (wide[0] == 7).all() and (wide[51] == 7).all()
+    scratch = torch.full((B.smoe_mx_product_bytes(2100, 3, 6, 64),), 255, dtype=torch.uint8, device="cuda")
+    wide = torch.full((2102, 3, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = B.smoe_mx_product(ctx, W, X, idx=i, scratch=scratch, y=wide[1:2101])
+    assert got.data_ptr() == wide[1:2101].data_ptr() and torch.equal(got, want)
+    assert (wide[0] == 7).all() and (wide[2101] == 7).all()
     with pytest.raises(B.SmoeError):
         B.smoe_mx_product(ctx, W, X, idx=i, scratch=scratch[:1024])
     assert B.smoe_mx_product(ctx, W, B.Mx(X.codes[:0], X.scales[:0]), idx=i[:0]).shape == (0, 3, 64)
     flat = B.Mx(W.codes[2], W.scales[2])
-    assert torch.equal(B.smoe_mx_product(ctx, flat, X), B.smoe_mx_product(ctx, W, X, idx=torch.full((50, 1), 2, dtype=torch.int32, device="cuda")))
+    assert torch.equal(B.smoe_mx_product(ctx, flat, X), B.smoe_mx_product(ctx, W, X, idx=torch.full((2100, 1), 2, dtype=torch.int32, device="cuda")))
 
 
 MATVECS = [(1, 1, 1, 16, 32), (1, 6, 64, 64, 2048), (16, 1, 1, 48, 1408), (16, 16, 5, 32, 96), (5, 3, 9, 16, 160), (7, 2, 2, 208, 544), (16, 6, 64, 32, 128), (2, 4, 4, 16, 65536)]

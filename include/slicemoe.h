@@ -316,8 +316,9 @@ int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_d
                     int k, const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, int x_slots, const int32_t* idx_dev,
                     int swiglu, int out_dtype, void* scratch_dev, size_t scratch_bytes, void* y_dev);
 /* The same for decode steps of T <= 16 tokens, x_dev [T,K] or [T,k,K] of act_dtype taken as it is (not quantised),
- * y_dev of act_dtype.  Every product of a weight and an activation is exact before the fp32 sum.  No scratch, one launch.  y_dev must
- * not overlap x_dev. */
+ * y_dev of act_dtype.  Every product of a weight and an activation is exact before the fp32 sum, but a weight of 2^128 or more
+ * (possible with scale bytes 253 and 254) makes its sum infinite or NaN, and what an fp32 activation holds below 2^-133
+ * counts as zero.  No scratch, one launch.  y_dev must not overlap x_dev. */
 int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
                    int k, const void* x_dev, int act_dtype, int x_slots, const int32_t* idx_dev, int swiglu,
                    void* y_dev);

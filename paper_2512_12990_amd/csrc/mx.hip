@@ -95,9 +95,9 @@ extern "C" int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const ui
 // byte is read once however many tokens share it.  Work-groups go by slots (that of a slot that is not the first of its expert has
 // nothing to do) or, with fewer experts than slots, by experts.  Its four or eight waves share the columns out, 128 at a time (32 columns of a row are one 16-byte load of a lane), and add their
 // sums up through LDS.
-//   Codes are expanded to bf16, which holds e2m1 times a power of two exactly, and multiplied by matrix instructions with
+//   Codes are expanded to bf16, which holds e2m1 times a power of two exactly (below 2^128; infinite from there on), and multiplied by matrix instructions with
 // fp32 sums.  fp32 activations go in as three bf16 numbers whose sum they are (8 + 8 + 8 bits, cut off, not rounded), so
-// these products are exact too; the splitting is seven vector instructions a number, which is why it serves RT tiles of rows at once.
+// these products are exact too (bits below 2^-133, bf16's smallest, are cut off); the splitting is seven vector instructions a number, which is why it serves RT tiles of rows at once.
 struct MatvecArgs {
   const uint8_t* codes; const uint8_t* scales; const void* x; const int32_t* idx; void* y;
   int E, N, K, T, k, x_slots, swiglu, by_expert;

@@ -461,6 +461,34 @@ def test_mx_matvec_scales(ctx):
     assert np.isnan(want[:, 0, 3]).all()
 
 
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 4])
+def test_mx_matvec_ends_of_the_range(ctx, T, act):
+    """Every code at the largest and smallest scales; activations down to the smallest."""
+    N, K = 16, 64
+    codes, scales = np.zeros((1, N, K // 2), np.uint8), np.full((1, N, 2), 127, np.uint8)
+    codes[0, :, 0] = np.arange(16)                           # row n: code n at column 0
+    for byte in (0, 1, 127, 250, 252, 253, 254):
+        scales[0, :, 0] = byte
+        W = B.Mx(dev(codes), dev(scales))
+        w = O.mx_values(codes, scales)[0, :, 0]
+        inf = np.abs(w) >= 2.0 ** 128
+        for e in (-149, -133, -120, -110, 0, 100):
+            x = torch.zeros(T, K)
+            x[:, 0] = torch.tensor(1.5 + 2.0 ** -10 + 2.0 ** -23) * 2.0 ** max(e, -126) * 2.0 ** min(e + 126, 0)
+            x = x.to(DT[act])
+            want = np64(x)[0, 0] * w
+            over = np.abs(want) > 3.3e38                     # (mantissas 1.5 and 2.25: none close to 2^128)
+            # two additions (up to a step each), the activation's lost bits (bf16 has none there), the result's rounding and its smallest step
+            tol = np.abs(want) * (4 * U32 + HALF[act]) + np.abs(w) * (2.0 ** -133 if act == "f32" else 0) + 2.0 ** (-133 if act == "bf16" else -149)
+            got = np64(B.smoe_mx_matvec(ctx, W, x.cuda())).reshape(T, N)
+            for row in got:
+                assert not np.isfinite(row[inf]).any(), (byte, e)
+                assert np.array_equal(row[over & ~inf], np.sign(want[over & ~inf]) * np.inf), (byte, e)
+                fine = ~over & ~inf
+                assert (np.abs(row - want)[fine] <= tol[fine]).all(), (byte, e)
+
+
 @pytest.mark.parametrize("T", [1, 5])
 def test_matvec_against_product(ctx, T):
     """Activations that quantise without loss: both products see the same numbers."""

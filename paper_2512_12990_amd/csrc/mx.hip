@@ -297,8 +297,8 @@ extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t*
   const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu, T > 1 && E < T * k};
   // Rows of a work-group.  Four tiles share one fetch and one splitting of the activations between four waves, one unit of columns in flight each, so that many
   // work-groups fit a CU; where that leaves too few work-groups, one tile and eight waves.  Microseconds with four tiles / with one: 16 tokens, top-6 of 64, N 2048,
-  // K 1408, fp32 30 / 62; 16 tokens, N 21888, K 2048, bf16 (342 work-groups) 15.0 / 18.9; 4 tokens, top-4 of 60, N 2816, K 2048 (704) 17.6 / 20.0; one token, top-6, the
-  // same matrices (264) 11.8 / 9.8; one token, dense, N 8192, K 8192 (128) 19.5 / 14.4, N 2048, K 10944 (32) 21.9 / 8.0; fp32, one token, top-6, N 2048, K 1408 (192) 8.4 / 8.7.
+  // K 1408, fp32 29 / 65; 16 tokens, N 21888, K 2048, bf16 (342 work-groups) 13.7 / 18.4; 4 tokens, top-4 of 60, N 2816, K 2048 (704) 16.0 / 18.5; one token, top-6, the
+  // same matrices (264) 11.2 / 9.6; one token, dense, N 8192, K 8192 (128) 19.1 / 13.5, N 2048, K 10944 (32) 19.7 / 7.8; fp32, one token, top-6, N 2048, K 1408 (192) 7.3 / 7.7.
   const long long wgs = (long long)((N + 63) / 64) * (!idx_dev ? 1 : T * k < E ? T * k : E);
   if (act_dtype == SMOE_F32) {
     if (wgs < 128) launch_matvec<SMOE_F32, 1, 8>(ctx, a);

@@ -1,0 +1,81 @@
+"""Score routing, residual norm and microscaled products where numbers, sizes and kernel variants reach their ends."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_12990_amd import binding as B
+from test_gpu_block_ops import DT, HALF, U32, dev, np64
+
+pytestmark = pytest.mark.gpu
+
+TINY = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133}      # smallest step of the type
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Ctx(0, workspace_bytes=0)
+    yield c
+    c.close()
+
+
+# ------------------------------------------------------------------------------------------ SwiGLU
+UPS = np.array([1.0, -1.0, 1.5e10, -2.5e20, 1.25e30, 3e38, 1e-20, -3e38])
+GATES = np.array([-60, -75.9, -76.1, -76.3, -80, -86, -87.2, -87.5, -88, -88.6, -88.8, -89, -95, -100, -104, -110,
+                  -120, -130, -140, -150, -160, -170, -175, -180, -185, -190, -195, -200, -206, -210, -250, -3e38])
+
+
+def check_swiglu(got, g, u, out):
+    """silu(g) * u; the kernel's own bound is 9 half steps of fp32, and the result is rounded once more."""
+    g, u = np.broadcast_arrays(g, u)
+    with np.errstate(over="ignore"):
+        want = g / (1.0 + np.exp(-g)) * u
+    tol = np.abs(want) * (9 * U32 + HALF[out]) + TINY[out]
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), [(float(a), float(b), float(c), float(d)) for a, b, c, d in zip(g[bad], u[bad], got[bad], want[bad])][:5]
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_matvec_swiglu_far_below_zero(ctx, act):
+    """Gates from -60 on down: silu(g) is no fp32 number there or a subnormal one, silu(g) * u still is."""
+    N, K = 16, 32
+    codes = np.zeros((1, N, K // 2), np.uint8)
+    codes[0, 0::2, 0] = 2                                    # every gate row: weight 1 at column 0
+    for i in range(8):
+        codes[0, 2 * i + 1, (8 + i) // 2] = 2 << (4 * (i % 2))      # up row i: weight 1 at column 8 + i
+    W = B.Mx(dev(codes), dev(np.full((1, N, 1), 127, np.uint8)))
+    for at in (0, 16):
+        x = torch.zeros(16, K, dtype=torch.float64)
+        x[:, 0] = torch.from_numpy(GATES[at:at + 16])
+        x[:, 8:16] = torch.from_numpy(UPS)
+        x = x.to(DT[act])
+        got = np64(B.smoe_mx_matvec(ctx, W, x.cuda(), swiglu=True))[:, 0]
+        x = np64(x)
+        check_swiglu(got, x[:, :1], x[:, 8:16], act)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_product_swiglu_far_below_zero(ctx, out):
+    """The same in the product of quantised numbers: a gate is the sum of codes times 16 and of codes times a half."""
+    grid = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])
+    gates = [((4, 1, 0), (0, 0)), ((4, 1, .5), (0, 0)), ((4, 1.5, 0), (0, 0)), ((4, 1.5, 0), (1.5, 0)), ((4, 1.5, 0), (2, 0)), ((6, 0, 0), (0, 0)),
+             ((6, 1.5, 0), (0, 0)), ((6, 3, 0), (1, 0)), ((6, 4, 1), (3, 0)), ((6, 6, 0), (0, 0)), ((6, 6, .5), (4, 1)), ((6, 6, 6), (0, 0))]
+    ups = [(1, 127), (1.5, 127 + 30), (-6, 127 + 60), (3, 127 + 100), (-4, 127 + 120), (1, 127 - 60)]
+    code = lambda v: int(np.nonzero(grid == abs(v))[0][0]) + (8 if v < 0 else 0)
+    N, K = 16, 96
+    wn = np.zeros((N, K), np.uint8)                          # codes, one a column
+    wn[0::2, [0, 1, 2, 32, 33]] = 2
+    wn[1::2, 64] = 2
+    xn, xs, g, u = [], [], [], []
+    for coarse, fine in gates:
+        for v, byte in ups:
+            row = np.zeros(K, np.uint8)
+            row[:3], row[32:34], row[64] = [code(-c) for c in coarse], [code(-c) for c in fine], code(v)
+            xn.append(row)
+            xs.append([131, 126, byte])
+            g.append(-16.0 * sum(coarse) - 0.5 * sum(fine))
+            u.append(v * 2.0 ** (byte - 127))
+    pack = lambda n: np.ascontiguousarray(n[..., 0::2] | (n[..., 1::2] << 4))
+    W = B.Mx(dev(pack(wn)), dev(np.full((N, 3), 127, np.uint8)))
+    X = B.Mx(dev(pack(np.stack(xn))), dev(np.array(xs, np.uint8)))
+    got = np64(B.smoe_mx_product(ctx, W, X, swiglu=True, out_dtype=DT[out]))[:, 0]
+    check_swiglu(got, np.array(g)[:, None] + np.zeros((1, 8)), np.array(u)[:, None] + np.zeros((1, 8)), out)

@@ -31,9 +31,9 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float* red
 template <int ACT, int RES, int NT, int NC>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void residual_norm_kernel(NormArgs a) {
   __shared__ float red[2 * (NT / 64)];
-  const int t = NT == 64 ? (int)blockIdx.x * 4 + (threadIdx.x >> 6) : (int)blockIdx.x;
+  const int t = NT == 64 ? row_group() * 4 + (threadIdx.x >> 6) : row_group();
   const int tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
-  if (NT == 64 && t >= a.T) return;                     // (whole waves; no barrier in this form)
+  if (t >= a.T) return;                                 // (whole waves, and no barrier, or whole work-groups)
   const int d = a.d;
   const float inv_d = 1.0f / (float)d;
   const size_t row = (size_t)t * d;
@@ -120,11 +120,11 @@ template <int ACT, int RES>
 static int launch_norm(smoe_ctx* ctx, const NormArgs& a) {
   const int pieces = a.d / 8;
   hipStream_t st = ctx->stream;
-  if (pieces <= 64) residual_norm_kernel<ACT, RES, 64, 1><<<(a.T + 3) / 4, 256, 0, st>>>(a);
-  else if (pieces <= 256) residual_norm_kernel<ACT, RES, 256, 1><<<a.T, 256, 0, st>>>(a);
-  else if (pieces <= 512) residual_norm_kernel<ACT, RES, 256, 2><<<a.T, 256, 0, st>>>(a);
-  else if (pieces <= 1024) residual_norm_kernel<ACT, RES, 512, 2><<<a.T, 512, 0, st>>>(a);
-  else residual_norm_kernel<ACT, RES, 1024, 2><<<a.T, 1024, 0, st>>>(a);
+  if (pieces <= 64) residual_norm_kernel<ACT, RES, 64, 1><<<grid_of((a.T + 3) / 4), 256, 0, st>>>(a);
+  else if (pieces <= 256) residual_norm_kernel<ACT, RES, 256, 1><<<grid_of(a.T), 256, 0, st>>>(a);
+  else if (pieces <= 512) residual_norm_kernel<ACT, RES, 256, 2><<<grid_of(a.T), 256, 0, st>>>(a);
+  else if (pieces <= 1024) residual_norm_kernel<ACT, RES, 512, 2><<<grid_of(a.T), 512, 0, st>>>(a);
+  else residual_norm_kernel<ACT, RES, 1024, 2><<<grid_of(a.T), 1024, 0, st>>>(a);
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;
 }

@@ -79,3 +79,33 @@ def test_product_swiglu_far_below_zero(ctx, out):
     X = B.Mx(dev(pack(np.stack(xn))), dev(np.array(xs, np.uint8)))
     got = np64(B.smoe_mx_product(ctx, W, X, swiglu=True, out_dtype=DT[out]))[:, 0]
     check_swiglu(got, np.array(g)[:, None] + np.zeros((1, 8)), np.array(u)[:, None] + np.zeros((1, 8)), out)
+
+
+# ------------------------------------------------------------------------------------ largest launches
+def room_for(nbytes):
+    """Skips where the device has not that much free memory."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nbytes:
+        pytest.skip("needs %d GB of free device memory" % (nbytes >> 30))
+
+
+@pytest.mark.parametrize("T, d", [(1 << 22, 8200), ((1 << 20) + 3, 8200), ((1 << 20) + 1, 520), (1 << 22, 512)])
+def test_residual_norm_most_rows(ctx, T, d):
+    """Work-groups in several rows of a grid: every token is served once, the last ones too."""
+    room_for(T * d * 4 + (8 << 30))
+    res = torch.ones((T, d), dtype=torch.bfloat16, device="cuda")
+    at = sorted({0, 1, (1 << 20) - 1, 1 << 20, T // 2 + 5, T - 2, T - 1} & set(range(T)))
+    rows = torch.randn((len(at), d), generator=torch.Generator().manual_seed(d)).bfloat16()
+    res[torch.tensor(at, device="cuda")] = rows.cuda()
+    out, x = B.smoe_residual_norm(ctx, res, res_out=res)
+    assert out is res
+    i = torch.tensor(at, device="cuda")
+    want = np64(rows)
+    assert np.array_equal(np64(res[i]), want)
+    # sum of squares: at most 54 roundings, halved by the root, and 4 of mean, eps, root and division; then the result's own and the type's
+    want = want / np.sqrt((want * want).mean(-1, keepdims=True) + 1e-6)
+    got = np64(x[i])
+    assert (np.abs(got - want) <= np.abs(want) * (33 * U32 + HALF["bf16"])).all()
+    x[i] = 1.0                                               # everywhere else 1 / sqrt(1 + 1e-6) is 1 in bfloat16
+    for a in range(0, T, 1 << 18):
+        assert (x[a:a + (1 << 18)] == 1.0).all()

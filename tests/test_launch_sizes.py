@@ -1,0 +1,87 @@
+"""Sizes of kernel launches at the ends of the documented ranges, on the CPU: the HIP calls that a launch makes are replaced by ones that
+record it.  A launch takes fewer than 2^32 threads along each axis and at most 1024 in a work-group."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2512_12990_amd import binding as B
+
+SHIM = r"""
+#include <stddef.h>
+#include <stdint.h>
+typedef struct { uint32_t x, y, z; } dim3;
+static dim3 g_grid, g_block;
+static uint32_t g_log[64][6];
+static int g_n;
+int launches(uint32_t* out) { int n = g_n; for (int i = 0; i < n; i++) for (int j = 0; j < 6; j++) out[6 * i + j] = g_log[i][j]; g_n = 0; return n; }
+int __hipPushCallConfiguration(dim3 g, dim3 b, size_t lds, void* s) { g_grid = g; g_block = b; return 0; }
+int __hipPopCallConfiguration(dim3* g, dim3* b, size_t* lds, void** s) { *g = g_grid; *b = g_block; *lds = 0; *s = 0; return 0; }
+int hipLaunchKernel(const void* f, dim3 g, dim3 b, void** args, size_t lds, void* s) {
+  if (g_n < 64) { uint32_t v[6] = {g.x, g.y, g.z, b.x, b.y, b.z}; for (int j = 0; j < 6; j++) g_log[g_n][j] = v[j]; g_n++; }
+  return 0;
+}
+int hipGetLastError(void) { return 0; }
+int hipGetDevice(int* d) { *d = 0; return 0; }
+int hipSetDevice(int d) { return 0; }
+int hipFuncSetAttribute(const void* f, int a, int v) { return 0; }
+"""
+
+RUN = r"""
+import ctypes as C, json, sys
+shim = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)              # found before the HIP runtime that the library links
+lib = C.CDLL(sys.argv[2])
+signatures, calls = json.loads(sys.argv[3])
+ct = {"p": C.c_void_p, "i": C.c_int, "l": C.c_longlong, "f": C.c_float, "z": C.c_size_t}
+ctx = C.c_void_p()
+assert lib.smoe_ctx_create(0, None, None, C.c_size_t(0), C.byref(ctx)) == 0
+log, out = (C.c_uint32 * 384)(), []
+for name, args in calls:
+    f = getattr(lib, name)
+    f.argtypes = [ct[c] for c in signatures[name]]
+    rc = f(ctx, *args)
+    n = shim.launches(log)
+    out.append((rc, [list(log[6 * i:6 * i + 6]) for i in range(n)]))
+print(json.dumps(out))
+"""
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    d = tmp_path_factory.mktemp("shim")
+    src, so = str(d / "shim.c"), str(d / "shim.so")
+    with open(src, "w") as f:
+        f.write(SHIM)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-o", so, src], check=True)
+
+    def run(calls):
+        arg = json.dumps(({n: B._SIGNATURES[n] for n, _ in calls}, calls))
+        r = subprocess.run([sys.executable, "-c", RUN, so, os.path.abspath(B.LIB_PATH), arg], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr
+        return json.loads(r.stdout)
+    return run
+
+
+P = 1 << 20                      # an aligned address that no kernel gets to see
+BIG = 1 << 22
+
+
+def check(launches, calls):
+    """Every call is accepted and its launches fit; the number of work-groups of each call's last launch."""
+    n = []
+    for (name, args), (rc, log) in zip(calls, launches(calls)):
+        assert rc == 0 and log, (name, args, rc)
+        for gx, gy, gz, bx, by, bz in log:
+            assert max(gx * bx, gy * by, gz * bz) < 1 << 32 and min(gx, gy, gz) > 0 and bx * by * bz <= 1024, (name, args, log)
+        n.append(gx * gy * gz)
+    return n
+
+
+@pytest.mark.parametrize("T", [1, 5, BIG - 1, BIG])
+def test_residual_norm(launches, T):
+    calls = [["smoe_residual_norm", [T, d, 0, None, None, None, None, 0, 1.0, P, None, 1e-6, act, res, 2 * P, 3 * P]]
+             for d in (8, 512, 520, 2048, 2056, 4096, 4104, 8192, 8200, 16384) for act in (0, 1) for res in (0, 1)]
+    for (_, args), n in zip(calls, check(launches, calls)):
+        assert n * (4 if args[1] <= 512 else 1) >= T         # four rows a work-group, or one

@@ -109,3 +109,23 @@ def test_residual_norm_most_rows(ctx, T, d):
     x[i] = 1.0                                               # everywhere else 1 / sqrt(1 + 1e-6) is 1 in bfloat16
     for a in range(0, T, 1 << 18):
         assert (x[a:a + (1 << 18)] == 1.0).all()
+
+
+@pytest.mark.parametrize("T, d, act", [(1 << 22, 7400, "f32"), ((1 << 20) + 3, 14700, "bf16"), ((1 << 21) + 5, 6000, "f32")])
+def test_route_scores_from_activations_most_tokens(ctx, T, d, act):
+    """One or two wide tokens to a work-group, and work-groups in several rows of a grid."""
+    size = T * d * (4 if act == "f32" else 2)
+    room_for(size + (4 << 30))
+    x = torch.zeros((T, d), dtype=DT[act], device="cuda")
+    at = sorted({0, 1, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T // 2 + 5, T - 2, T - 1} & set(range(T)))
+    x[torch.tensor(at, device="cuda"), 3] = 1.0
+    wr = torch.zeros((3, d), device="cuda")
+    wr[:, 3] = torch.tensor([0.0, 1.0, 3.0])                 # logits 0 everywhere (a tie: expert 0, then 1), or 0, 1, 3
+    idx, w = B.smoe_route_scores(ctx, 2, x=x, w_router=wr, score="softmax")
+    del x
+    other = torch.ones(T, dtype=torch.bool, device="cuda")
+    other[torch.tensor(at, device="cuda")] = False
+    assert (idx[other] == torch.tensor([0, 1], device="cuda")).all() and (w[other] == torch.tensor(1.0 / 3.0)).all()
+    s = np.exp([0.0, 1.0, 3.0]) / np.exp([0.0, 1.0, 3.0]).sum()
+    assert (idx[~other] == torch.tensor([2, 1], device="cuda")).all()
+    assert (np.abs(np64(w[~other]) - s[[2, 1]]) <= s[[2, 1]] * 2 * U32).all()

@@ -85,3 +85,17 @@ def test_residual_norm(launches, T):
              for d in (8, 512, 520, 2048, 2056, 4096, 4104, 8192, 8200, 16384) for act in (0, 1) for res in (0, 1)]
     for (_, args), n in zip(calls, check(launches, calls)):
         assert n * (4 if args[1] <= 512 else 1) >= T         # four rows a work-group, or one
+
+
+@pytest.mark.parametrize("T", [1, 300, 600, 2047, BIG - 1, BIG])
+def test_route_scores(launches, T):
+    def call(E, k, d, logits, act, ng=1):
+        return ["smoe_route_scores", [T, E, k, d, P if logits else None, None if logits else P, act, None if logits else P, 1, ng, ng, 1, None, 1, 1.0, P, P]]
+    given = [call(E, 4, 0, True, 0, ng) for E, ng in ((4, 1), (60, 1), (63, 1), (64, 8), (128, 8), (160, 8), (200, 1), (256, 1), (256, 64))]
+    for n in check(launches, given):
+        assert n * 16 >= T                                   # four waves of four tokens or of one
+    # widths on both sides of where 8, 4, 2 tokens and 1 still fit a work-group
+    work = [call(E, 1, d, False, act) for E in (1, 64, 256) for act in (0, 1) for d in (64, 1500, 3400, 3700, 6500, 7400, 12000, 13600)]
+    work += [call(E, 1, d, False, 1) for E in (1, 64, 256) for d in (14700, 24000, 27000)]
+    for n in check(launches, work):
+        assert n * 8 >= T

@@ -99,3 +99,24 @@ def test_route_scores(launches, T):
     work += [call(E, 1, d, False, 1) for E in (1, 64, 256) for d in (14700, 24000, 27000)]
     for n in check(launches, work):
         assert n * 8 >= T
+
+
+def test_mx_quantize(launches):
+    calls = [[n, [rows, K, P, 0, P, P] if n == "smoe_mx_quantize" else [rows, K, P, P, P, 1]]
+             for rows, K in ((1, 32), (3, 96), (1 << 29, 32), (1 << 18, 1 << 16), ((1 << 34) // 96, 96)) for n in ("smoe_mx_quantize", "smoe_mx_dequantize")]
+    for (_, args), n in zip(calls, check(launches, calls)):
+        assert n * 256 * 8 >= args[0] * args[1]
+
+
+def test_mx_product(launches):
+    calls = [["smoe_mx_product", [E, N, K, P, P, T, k, P, P, slots, P if E > 1 or k > 1 else None, 1, 0, P, 1 << 40, P]]
+             for T, k, E, N, K, slots in ((1, 1, 1, 16, 32, 0), (1, 16, 256, 1 << 20, 32, 0), (BIG, 1, 1, 8192, 32, 0), (BIG, 1, 256, 8192, 32, 0), (1 << 18, 16, 256, 8192, 64, 1),
+                                          (2048, 16, 256, 1 << 20, 4064, 0), (32768, 1, 1, 1 << 20, 4064, 0), (BIG, 1, 3, 16, 992, 0), (16, 1, 256, 1 << 20, 4064, 0), (100, 2, 256, 65536, 65504, 1))]
+    check(launches, calls)
+
+
+def test_mx_matvec(launches):
+    calls = [["smoe_mx_matvec", [E, N, K, P, P, T, k, P, act, 0, P if E > 1 or k > 1 else None, 0, 2 * P]]
+             for T, k, E, N, K in ((1, 1, 1, 16, 32), (16, 16, 256, 1 << 20, 4064), (16, 1, 1, 1 << 20, 4064), (1, 16, 256, 1 << 20, 32), (16, 16, 3, 65504, 65536), (5, 1, 256, 48, 65536))
+             for act in (0, 1)]
+    check(launches, calls)

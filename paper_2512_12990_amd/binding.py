@@ -349,7 +349,8 @@ GROUP_SCORES = {"max": 0, "top2": 1}
 _ACTS = {torch.float32, torch.bfloat16}
 _F32, _BF16, _I32, _U8 = {torch.float32}, {torch.bfloat16}, {torch.int32}, {torch.uint8}
 _ONE = {torch.float32: _F32, torch.bfloat16: _BF16}
-_stream_now = torch._C._cuda_getCurrentRawStream
+# the current stream's address; the public call, which builds an object, where torch (without GPU support) lacks the shorter one
+_stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _empty = torch.empty
 
 

@@ -374,7 +374,7 @@ def _tensors(values):
     for v in values:
         if isinstance(v, torch.Tensor):
             yield v
-        elif isinstance(v, tuple):
+        elif isinstance(v, (tuple, list)):
             yield from _tensors(v)
 
 

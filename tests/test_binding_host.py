@@ -2,6 +2,8 @@
 import subprocess
 import sys
 
+import torch
+
 from paper_2512_12990_amd import binding as B
 
 
@@ -21,3 +23,10 @@ print("fine")
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "fine", r.stderr
+
+
+def test_tensors_of_a_call():
+    """Every tensor that a call is given has to be found, whatever the pair of an Mx arrives in: it is kept from reuse while another stream works on it."""
+    a, b, c, d, e = (torch.zeros(1) for _ in range(5))
+    got = list(B._tensors((a, B.Mx(b, c), 3, None, [d, e], "x")))
+    assert [id(t) for t in got] == [id(t) for t in (a, b, c, d, e)]

@@ -21,7 +21,7 @@ ROOT = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, ROOT)
 
 HBM_PEAK_GBPS = 8000.0
-
+FP4_PEAK_TFLOPS = 10000.0      # 4-bit matrix instructions, dense: four times bf16
 
 PLANE_BITS = 4      # bits per code in a plane: 4 for the 8/4 nest, 3 for 6/3 (--nest 63), 2 for 4/2 (--nest 42)
 
@@ -488,64 +488,80 @@ def prefill_bench(args):
     print(json.dumps(out))
 
 
+def mxfp4_roofline(nbytes, flops, us):
+    """Of a block that has to read `nbytes` of weights and multiply `flops`: the resource that takes longer at its peak, and how near `us` comes to that."""
+    hbm = {"bound": "hbm", "achieved": nbytes / us / 1e3, "peak": HBM_PEAK_GBPS, "unit": "GB/s"}
+    mfma = {"bound": "mfma", "achieved": flops / us / 1e6, "peak": FP4_PEAK_TFLOPS, "unit": "TFLOP/s"}
+    r = max(hbm, mfma, key=lambda m: m["achieved"] / m["peak"])
+    r["frac"] = r["achieved"] / r["peak"]
+    return r
+
+
 def mxfp4_block_bench(args):
     """One MoE block around MXFP4 experts (64 routed, d_model 2048, d_ff 1408, top-6): norm of the residual stream, sigmoid routing in 8
     groups with a balance bias, gate/up product with SwiGLU, down product, and the residual norm that joins the slots.  --tokens (1 to 16) as
-    a decode step, --prefill-tokens as a prompt with quantised activations.  A step is one such block, replayed from a HIP graph."""
+    a decode step, --prefill-tokens as a prompt with quantised activations.  A step is one such block, replayed from a HIP graph; the steps go round over
+    four layers' weights (1.2 GB, where the last-level cache holds 256 MB) and, in decode, eight sets of tokens for each, so that weights come from HBM."""
     import torch
     from paper_2512_12990_amd import binding as B, synth
     wl = synth.DSV2_LAYER
     E, d, f, k = wl.layer.n_experts, wl.layer.d_model, wl.layer.d_ff, wl.layer.top_k
     T, few, dev = args.prefill_tokens or args.tokens, not args.prefill_tokens, "cuda:0"
+    n_layers, n_blocks = 4, 32 if few else 4
     s = torch.cuda.Stream()
     ctx = B.Ctx(0, stream=s)
     with torch.cuda.stream(s):
-        up, down = [], []
-        for e in range(E):
-            wg, wu, wd = synth.expert_weights(wl.seed, 0, e, d, f, "bf16", dev)
-            up.append(torch.stack([wg, wu], 1).reshape(2 * f, d))          # gate and up rows in turn
-            down.append(wd)
-        up, down = (B.smoe_mx_quantize(ctx, torch.stack(w)) for w in (up, down))
-        h = synth.activations(wl.seed, T, d, "f32").to(dev)
-        wr, bias = synth.router_weight(wl.seed, 0, E, d).to(dev), torch.zeros(E, device=dev)
+        layers = []
+        for layer in range(n_layers):
+            up, down = [], []
+            for e in range(E):
+                wg, wu, wd = synth.expert_weights(wl.seed, layer, e, d, f, "bf16", dev)
+                up.append(torch.stack([wg, wu], 1).reshape(2 * f, d))          # gate and up rows in turn
+                down.append(wd)
+            layers.append((*(B.smoe_mx_quantize(ctx, torch.stack(w)) for w in (up, down)), synth.router_weight(wl.seed, layer, E, d).to(dev)))
+        hs = synth.activations(wl.seed, n_blocks * T, d, "f32").to(dev).reshape(n_blocks, T, d)
+        bias = torch.zeros(E, device=dev)
         one = torch.ones(d, dtype=torch.bfloat16, device=dev)
 
-        def step():
-            _, x = B.smoe_residual_norm(ctx, h, pre_w=one)
+        def step(i):
+            up, down, wr = layers[i % n_layers]
+            _, x = B.smoe_residual_norm(ctx, hs[i], pre_w=one)
             idx, w = B.smoe_route_scores(ctx, k, x=x, w_router=wr, score="sigmoid", n_group=8, topk_group=4, group_score="top2", bias=bias, norm_topk=True)
             if few:
                 y = B.smoe_mx_matvec(ctx, down, B.smoe_mx_matvec(ctx, up, x, idx=idx, swiglu=True), idx=idx)
             else:
                 mid = B.smoe_mx_product(ctx, up, B.smoe_mx_quantize(ctx, x), idx=idx, swiglu=True)
                 y = B.smoe_mx_product(ctx, down, B.smoe_mx_quantize(ctx, mid), idx=idx)
-            return B.smoe_residual_norm(ctx, h, y=y, slot_w=w, pre_w=one), idx
+            return B.smoe_residual_norm(ctx, hs[i], y=y, slot_w=w, pre_w=one), idx
 
-        _, idx = step()
+        used = sum(int(torch.unique(step(i)[1]).numel()) for i in range(n_blocks)) / n_blocks
     torch.cuda.synchronize()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph, stream=s):
-        step()
+    graphs = []
+    for i in range(n_blocks):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            step(i)
     steps = min(args.steps, 1024 if few else 50)
     ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     with torch.cuda.stream(s):
-        for _ in range(args.warmup):
-            graph.replay()
+        for i in range(args.warmup):
+            graphs[i % n_blocks].replay()
         torch.cuda.synchronize()
         ev0.record(s)
-        for _ in range(steps):
-            graph.replay()
+        for i in range(steps):
+            graphs[i % n_blocks].replay()
         ev1.record(s)
     torch.cuda.synchronize()
     us = ev0.elapsed_time(ev1) / steps * 1e3
-    used = int(torch.unique(idx).numel())
     wbytes, flops = used * 3 * d * f * 17 / 32, 2.0 * T * k * 3 * d * f
     print(json.dumps({
         "metric": "MoE block us (%d tokens, norm + score routing + MXFP4 experts + residual norm)" % T, "value": us, "unit": "us/block", "n_gpus": 1, "steps": steps,
         "warmup": args.warmup, "ms_per_step": us / 1e3, "higher_is_better": False, "scaling": "weak", "vs_baseline": None,
         "dtype": "bf16 activations, MXFP4 weights" + ("" if few else " and products"), "data": "synthetic",
-        "config": {"workload": "DeepSeek-V2-Lite-shaped block, MXFP4 experts", "tokens": T, "n_experts": E, "top_k": k, "d_model": d, "d_ff": f, "experts_used": used},
-        "roofline": {"bound": "hbm", "achieved": wbytes / us / 1e3, "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": wbytes / us / 1e3 / HBM_PEAK_GBPS,
-                     "weight_bytes_per_step": wbytes, "flops_per_step": flops, "tflops": flops / us / 1e6}}))
+        "config": {"workload": "DeepSeek-V2-Lite-shaped block, MXFP4 experts", "tokens": T, "n_experts": E, "top_k": k, "d_model": d, "d_ff": f, "experts_used": used,
+                   "layers_in_rotation": n_layers},
+        "roofline": {**mxfp4_roofline(wbytes, flops, us), "weight_bytes_per_step": wbytes, "flops_per_step": flops, "weight_gbps": wbytes / us / 1e3,
+                     "tflops": flops / us / 1e6}}))
 
 
 def stack_bench(args):

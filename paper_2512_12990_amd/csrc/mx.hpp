@@ -12,23 +12,32 @@ __device__ __forceinline__ float mx_scale(uint32_t byte) {
   return __uint_as_float(u);
 }
 
-// silu(g) * u.  e^-g = 2^(t + r), t = -g log2 e rounded and r what that rounding left, so that the exponential keeps its last
-// bits at any g.  Below g = -76 (t > 110) 1 + e^-g is e^-g to the last bit but may pass fp32, and its reciprocal may be subnormal, where a large u still makes a
-// normal number of it: there m = 2^160 e^g stands for the quotient, and 2^-160 comes in two halves with u (which only a result of less than the smallest subnormal
-// can make subnormal).  The limits of +-220 keep infinities out of r; past them m is 0, and so is the result at any u (2^-317 * 2^128).  Off by at most 9 half
-// steps, and by a subnormal's step: exponential 4, sum 1, reciprocal 2, two products 2.
-__device__ __forceinline__ float swiglu(float g, float u) {
-  const float x = __builtin_amdgcn_fmed3f(-g, -220.0f, 220.0f);
+// silu(g) * u for gates from -76 on.  e^-g = 2^(t + r), t = -g log2 e rounded and r what that rounding left, so that the exponential keeps its last
+// bits at any g; the limits of +-200 keep infinities out of r.  Off by at most 9 half steps: exponential 4, sum 1,
+// reciprocal 2, two products 2.
+#define SWIGLU_FAR -76.0f
+__device__ __forceinline__ float swiglu_near(float g, float u) {
+  const float x = __builtin_amdgcn_fmed3f(-g, -200.0f, 200.0f);
   const float t = x * 1.44269502f, r = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -t));
-  const bool far = t > 110.0f;
-  float at;
+  const float e = __builtin_amdgcn_exp2f(t) * fmaf(r, 0.693147182f, 1.0f);
+  return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
+// For any gate.  Below -76 1 + e^-g is e^-g to the last bit but may pass fp32, and its reciprocal may be subnormal, where a large u still makes a normal
+// number of it: there m = 2^160 e^g stands for the quotient, and 2^-160 comes in two halves with u (which only a result of less than the smallest
+// subnormal can make subnormal).  Past the limit of -220 m is 0, and so is the result at any u (2^-317 * 2^128).  Off by fewer half steps, and by a
+// subnormal's step.
+__device__ __forceinline__ float swiglu(float g, float u) {
+  if (!(g < SWIGLU_FAR)) return swiglu_near(g, u);
+  const float x = fmaxf(g, -220.0f);
+  float t, at;
   {
 #pragma clang fp contract(off)
-    at = far ? 160.0f - t : t;                               // (exact; from x itself r would not be what is left)
+    t = x * 1.44269502f;
+    at = t + 160.0f;                                         // (exact; from x itself r would not be what is left)
   }
-  const float m = __builtin_amdgcn_exp2f(at) * fmaf(r, far ? -0.693147182f : 0.693147182f, 1.0f);
-  const float near_silu = g * __builtin_amdgcn_rcpf(1.0f + m);
-  return far ? u * 0x1p-80f * (g * m) * 0x1p-80f : near_silu * u;
+  const float r = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -t));
+  const float m = __builtin_amdgcn_exp2f(at) * fmaf(r, 0.693147182f, 1.0f);
+  return u * 0x1p-80f * (g * m) * 0x1p-80f;
 }
 
 // one expert's matrix [N, K]: byte offsets inside it stay below 2^31

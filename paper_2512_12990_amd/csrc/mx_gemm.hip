@@ -394,39 +394,48 @@ __device__ __forceinline__ void mx_gemm_tile(const MxGemmArgs& a, uint8_t* As) {
   const int n_out = sg ? a.N >> 1 : a.N, per_pass = a.out_f32 && !sg ? 1 : FN;                     // columns of Y; fragments at a time
   const int lpr = 31 - __builtin_clz((unsigned)(per_pass * (sg ? 16 : 32) * osz / 16));           // log2 of a row's 16-byte pieces
   uint8_t* o = As + wave * S::out_wave;
+  uint32_t low = 0;                                                    // lowest gate met, as bits: negative numbers are the larger the further they are from 0
+  auto write = [&](auto far_c) __attribute__((always_inline)) {
+    constexpr bool far = decltype(far_c)::value;
 #pragma unroll
-  for (int j = 0; j < FT; j++) {
-    const int r0 = (wt * FT + j) * 32;
-    if (r0 >= tile.count) continue;
+    for (int j = 0; j < FT; j++) {
+      const int r0 = (wt * FT + j) * 32;
+      if (r0 >= tile.count) continue;
 #pragma unroll
-    for (int i = 0; i < FN; i++) {
-      const int ip = per_pass == 1 ? 0 : i;                            // place of the fragment in the pass
+      for (int i = 0; i < FN; i++) {
+        const int ip = per_pass == 1 ? 0 : i;                            // place of the fragment in the pass
 #pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int nr = ip * 32 + 2 * r + 4 * h;
-        const float v0 = acc[i][j][r], v1 = acc[i][j][r + 1], v2 = acc[i][j][r + 2], v3 = acc[i][j][r + 3];
-        uint8_t* to = o + c * S::out_row;
-        if (sg) {
-          const float o0 = swiglu(v0, v1), o1 = swiglu(v2, v3);
-          if (a.out_f32) *(float2*)(to + (nr >> 1) * 4) = make_float2(o0, o1);
-          else *(uint32_t*)(to + (nr >> 1) * 2) = pack_bf16_rne(o0, o1);
-        } else {
-          if (a.out_f32) *(float4*)(to + nr * 4) = make_float4(v0, v1, v2, v3);
-          else *(uint2*)(to + nr * 2) = make_uint2(pack_bf16_rne(v0, v1), pack_bf16_rne(v2, v3));
+        for (int r = 0; r < 16; r += 4) {
+          const int nr = ip * 32 + 2 * r + 4 * h;
+          const float v0 = acc[i][j][r], v1 = acc[i][j][r + 1], v2 = acc[i][j][r + 2], v3 = acc[i][j][r + 3];
+          uint8_t* to = o + c * S::out_row;
+          if (sg) {
+            const float o0 = far ? swiglu(v0, v1) : swiglu_near(v0, v1), o1 = far ? swiglu(v2, v3) : swiglu_near(v2, v3);
+            if (!far) low = max(max(low, __float_as_uint(v0)), __float_as_uint(v2));
+            if (a.out_f32) *(float2*)(to + (nr >> 1) * 4) = make_float2(o0, o1);
+            else *(uint32_t*)(to + (nr >> 1) * 2) = pack_bf16_rne(o0, o1);
+          } else {
+            if (a.out_f32) *(float4*)(to + nr * 4) = make_float4(v0, v1, v2, v3);
+            else *(uint2*)(to + nr * 2) = make_uint2(pack_bf16_rne(v0, v1), pack_bf16_rne(v2, v3));
+          }
         }
-      }
-      if (ip == per_pass - 1) {
-        asm volatile("" ::: "memory");                                 // (LDS keeps a wave's accesses in order; so does the compiler now)
-        const int col0 = (n0 + (wn * FN + i - ip) * 32) >> sg;
-        for (int x = lane; x < 32 << lpr; x += 64) {
-          const int tr = x >> lpr, p = x & ((1 << lpr) - 1), col = col0 + p * (16 / osz);
-          if (r0 + tr < tile.count && col < n_out)                     // (N is a multiple of 16: sixteen bytes are in or out)
-            *(uint4*)((uint8_t*)a.y + ((size_t)slots[r0 + tr] * n_out + col) * osz) = *(const uint4*)(o + tr * S::out_row + p * 16);
+        if (ip == per_pass - 1) {
+          asm volatile("" ::: "memory");                                 // (LDS keeps a wave's accesses in order; so does the compiler now)
+          const int col0 = (n0 + (wn * FN + i - ip) * 32) >> sg;
+          for (int x = lane; x < 32 << lpr; x += 64) {
+            const int tr = x >> lpr, p = x & ((1 << lpr) - 1), col = col0 + p * (16 / osz);
+            if (r0 + tr < tile.count && col < n_out)                     // (N is a multiple of 16: sixteen bytes are in or out)
+              *(uint4*)((uint8_t*)a.y + ((size_t)slots[r0 + tr] * n_out + col) * osz) = *(const uint4*)(o + tr * S::out_row + p * 16);
+          }
+          asm volatile("" ::: "memory");
         }
-        asm volatile("" ::: "memory");
       }
     }
-  }
+  };
+  // The shorter form of the SwiGLU for all; a wave that met a gate below -76, as good as none, writes its results once more.  2048 tokens, top-4 of 60,
+  // N 2816, K 2048, on one machine each: 87.8 us against 87.1 with the shorter form alone; the longer form for all 89.2 against 83.2.
+  write(std::false_type{});
+  if (sg && __any(low > __float_as_uint(SWIGLU_FAR))) write(std::true_type{});
 }
 
 template <bool UNAL, int NT, int NN, int FT, int FN>

@@ -3,8 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import block_oracle as O
 from paper_2512_12990_amd import binding as B
-from test_gpu_block_ops import DT, HALF, U32, dev, np64
+from test_gpu_block_ops import DT, HALF, U32, dev, mx_random, np64
 
 pytestmark = pytest.mark.gpu
 
@@ -91,7 +92,7 @@ def room_for(nbytes):
 
 @pytest.mark.parametrize("T, d", [(1 << 22, 8200), ((1 << 20) + 3, 8200), ((1 << 20) + 1, 520), (1 << 22, 512)])
 def test_residual_norm_most_rows(ctx, T, d):
-    """Work-groups in several rows of a grid: every token is served once, the last ones too."""
+    """More rows than one launch takes: every token is served once, the last ones too."""
     room_for(T * d * 4 + (8 << 30))
     res = torch.ones((T, d), dtype=torch.bfloat16, device="cuda")
     at = sorted({0, 1, (1 << 20) - 1, 1 << 20, T // 2 + 5, T - 2, T - 1} & set(range(T)))
@@ -111,9 +112,27 @@ def test_residual_norm_most_rows(ctx, T, d):
         assert (x[a:a + (1 << 18)] == 1.0).all()
 
 
+@pytest.mark.parametrize("act, res", [("bf16", "f32"), ("f32", "bf16")])
+def test_residual_norm_most_rows_with_everything(ctx, act, res):
+    """Every operand moves on with the rows: the last rows are those of a call on them alone."""
+    T, d, k = (1 << 21) + 3, 16, 2
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")
+    y, w, gate, h = r(T, k, d).to(DT[act]), r(T, k), r(T, d).to(DT[act]), r(T, d).to(DT[res])
+    kw = dict(post_w=r(d).to(DT[act]), pre_w=r(d).to(DT[act]), scale=0.5)
+    out = B.smoe_residual_norm(ctx, h, y=y, slot_w=w, gate=gate, **kw)
+    for a, b in ((0, 8), ((1 << 20) - 8, 1 << 20), (1 << 20, (1 << 20) + 8), (T - 11, T)):
+        part = B.smoe_residual_norm(ctx, h[a:b].clone(), y=y[a:b].clone(), slot_w=w[a:b].clone(), gate=gate[a:b].clone(), **kw)
+        assert torch.equal(out[0][a:b], part[0]) and torch.equal(out[1][a:b], part[1])
+    kw["gate"] = gate[0]
+    out = B.smoe_residual_norm(ctx, h, y=y, slot_w=w, **kw)
+    part = B.smoe_residual_norm(ctx, h[-9:].clone(), y=y[-9:].clone(), slot_w=w[-9:].clone(), **kw)
+    assert torch.equal(out[0][-9:], part[0]) and torch.equal(out[1][-9:], part[1])
+
+
 @pytest.mark.parametrize("T, d, act", [(1 << 22, 7400, "f32"), ((1 << 20) + 3, 14700, "bf16"), ((1 << 21) + 5, 6000, "f32")])
 def test_route_scores_from_activations_most_tokens(ctx, T, d, act):
-    """One or two wide tokens to a work-group, and work-groups in several rows of a grid."""
+    """One or two wide tokens to a work-group, and more work-groups than one launch takes."""
     size = T * d * (4 if act == "f32" else 2)
     room_for(size + (4 << 30))
     x = torch.zeros((T, d), dtype=DT[act], device="cuda")
@@ -129,3 +148,42 @@ def test_route_scores_from_activations_most_tokens(ctx, T, d, act):
     s = np.exp([0.0, 1.0, 3.0]) / np.exp([0.0, 1.0, 3.0]).sum()
     assert (idx[~other] == torch.tensor([2, 1], device="cuda")).all()
     assert (np.abs(np64(w[~other]) - s[[2, 1]]) <= s[[2, 1]] * 2 * U32).all()
+
+
+# ------------------------------------------------------------------------------- formats, graphs
+def test_mx_dequantize_every_code_and_scale_to_bf16(ctx):
+    """A power of two with one more bit: exact in bfloat16 down to its subnormals, infinite from 2^128 on."""
+    codes = np.tile(np.arange(256, dtype=np.uint8).reshape(1, 16, 16), (256, 1, 1)).reshape(256, 256)
+    scales = np.repeat(np.arange(256, dtype=np.uint8)[:, None], 16, 1)
+    want = O.mx_values(codes, scales)
+    big = np.abs(want) >= 2.0 ** 128
+    want[big] = np.copysign(np.inf, want[big])
+    assert np.array_equal(np64(B.smoe_mx_dequantize(ctx, B.Mx(dev(codes), dev(scales)), torch.bfloat16)), want, equal_nan=True)
+
+
+def test_first_product_of_a_context_is_captured():
+    """A context's first call of the widest tile asks for its LDS while a graph is captured; replays on new contents, with eager work between them."""
+    rng = np.random.default_rng(2)
+    T, N, K = 4100, 2064, 128
+    w, x = mx_random(rng, N, K), mx_random(rng, T, K)
+    W, X = B.Mx(*map(dev, w)), B.Mx(*map(dev, x))
+    s = torch.cuda.Stream()
+    c = B.Ctx(0, stream=s, workspace_bytes=0)
+    y = torch.zeros((T, 1, N), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        B.smoe_mx_product(c, W, X, y=y)
+    for _ in range(3):
+        x = mx_random(rng, T, K)
+        X.codes.copy_(dev(x[0]))
+        X.scales.copy_(dev(x[1]))
+        y.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = O.product(O.mx_values(*w)[None], O.mx_values(*x), None, False)
+        assert torch.equal(y.cpu(), torch.from_numpy(want).float().bfloat16())
+        B.smoe_mx_quantize(c, torch.randn(64, 64, device="cuda"))
+        torch.cuda.synchronize()
+    c.close()

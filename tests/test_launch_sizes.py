@@ -1,5 +1,5 @@
 """Sizes of kernel launches at the ends of the documented ranges, on the CPU: the HIP calls that a launch makes are replaced by ones that
-record it.  A launch takes fewer than 2^32 threads along each axis and at most 1024 in a work-group."""
+record it.  A launch takes fewer than 2^32 threads along each axis, at most 1024 in a work-group and at most 160 KB of LDS."""
 import json
 import os
 import subprocess
@@ -7,6 +7,7 @@ import sys
 
 import pytest
 
+import block_cases
 from paper_2512_12990_amd import binding as B
 
 SHIM = r"""
@@ -14,13 +15,14 @@ SHIM = r"""
 #include <stdint.h>
 typedef struct { uint32_t x, y, z; } dim3;
 static dim3 g_grid, g_block;
-static uint32_t g_log[64][6];
+static size_t g_lds;
+static uint32_t g_log[64][7];
 static int g_n;
-int launches(uint32_t* out) { int n = g_n; for (int i = 0; i < n; i++) for (int j = 0; j < 6; j++) out[6 * i + j] = g_log[i][j]; g_n = 0; return n; }
-int __hipPushCallConfiguration(dim3 g, dim3 b, size_t lds, void* s) { g_grid = g; g_block = b; return 0; }
-int __hipPopCallConfiguration(dim3* g, dim3* b, size_t* lds, void** s) { *g = g_grid; *b = g_block; *lds = 0; *s = 0; return 0; }
+int launches(uint32_t* out) { int n = g_n; for (int i = 0; i < n; i++) for (int j = 0; j < 7; j++) out[7 * i + j] = g_log[i][j]; g_n = 0; return n; }
+int __hipPushCallConfiguration(dim3 g, dim3 b, size_t lds, void* s) { g_grid = g; g_block = b; g_lds = lds; return 0; }
+int __hipPopCallConfiguration(dim3* g, dim3* b, size_t* lds, void** s) { *g = g_grid; *b = g_block; *lds = g_lds; *s = 0; return 0; }
 int hipLaunchKernel(const void* f, dim3 g, dim3 b, void** args, size_t lds, void* s) {
-  if (g_n < 64) { uint32_t v[6] = {g.x, g.y, g.z, b.x, b.y, b.z}; for (int j = 0; j < 6; j++) g_log[g_n][j] = v[j]; g_n++; }
+  if (g_n < 64) { uint32_t v[7] = {g.x, g.y, g.z, b.x, b.y, b.z, (uint32_t)lds}; for (int j = 0; j < 7; j++) g_log[g_n][j] = v[j]; g_n++; }
   return 0;
 }
 int hipGetLastError(void) { return 0; }
@@ -37,13 +39,13 @@ signatures, calls = json.loads(sys.argv[3])
 ct = {"p": C.c_void_p, "i": C.c_int, "l": C.c_longlong, "f": C.c_float, "z": C.c_size_t}
 ctx = C.c_void_p()
 assert lib.smoe_ctx_create(0, None, None, C.c_size_t(0), C.byref(ctx)) == 0
-log, out = (C.c_uint32 * 384)(), []
+log, out = (C.c_uint32 * 448)(), []
 for name, args in calls:
     f = getattr(lib, name)
     f.argtypes = [ct[c] for c in signatures[name]]
     rc = f(ctx, *args)
     n = shim.launches(log)
-    out.append((rc, [list(log[6 * i:6 * i + 6]) for i in range(n)]))
+    out.append((rc, [list(log[7 * i:7 * i + 7]) for i in range(n)]))
 print(json.dumps(out))
 """
 
@@ -69,13 +71,13 @@ BIG = 1 << 22
 
 
 def check(launches, calls):
-    """Every call is accepted and its launches fit; the number of work-groups of each call's last launch."""
+    """Every call is accepted and its launches fit; the number of work-groups of each call's launches."""
     n = []
     for (name, args), (rc, log) in zip(calls, launches(calls)):
         assert rc == 0 and log, (name, args, rc)
-        for gx, gy, gz, bx, by, bz in log:
-            assert max(gx * bx, gy * by, gz * bz) < 1 << 32 and min(gx, gy, gz) > 0 and bx * by * bz <= 1024, (name, args, log)
-        n.append(gx * gy * gz)
+        for gx, gy, gz, bx, by, bz, lds in log:
+            assert max(gx * bx, gy * by, gz * bz) < 1 << 32 and min(gx, gy, gz) > 0 and bx * by * bz <= 1024 and lds <= 160 * 1024, (name, args, log)
+        n.append(sum(v[0] * v[1] * v[2] for v in log))
     return n
 
 
@@ -120,3 +122,29 @@ def test_mx_matvec(launches):
              for T, k, E, N, K in ((1, 1, 1, 16, 32), (16, 16, 256, 1 << 20, 4064), (16, 1, 1, 1 << 20, 4064), (1, 16, 256, 1 << 20, 32), (16, 16, 3, 65504, 65536), (5, 1, 256, 48, 65536))
              for act in (0, 1)]
     check(launches, calls)
+
+
+# ---------------------------------------------------------------- which variants the GPU tests' sizes reach
+def test_matvec_sizes_reach_both_forms(launches):
+    def forms(cases):
+        calls = [["smoe_mx_matvec", [E, N, K, P, P, T, k, P, act, 0, P if E > 1 or k > 1 else None, 0, 2 * P]] for T, k, E, N, K in cases for act in (0, 1)]
+        return {log[0][3] for _, log in launches(calls)}
+    assert forms(block_cases.MATVEC_FOUR_TILES) == {256} and forms(block_cases.MATVEC_ONE_TILE) == {512}
+
+
+def test_product_sizes_reach_every_tile(launches):
+    def forms(group, idx):
+        calls = [["smoe_mx_product", [E, N, K, P, P, T, k, P, P, 0, P if idx else None, 0, 0, P, 1 << 40, P]] for pair in group for T, k, E, N, K in pair]
+        return [(len(log), log[-1][3], log[-1][6]) for _, log in launches(calls)]
+    # six kernels: three shapes, which threads and LDS tell apart, of two alignments; a launch more where slots are listed before
+    search, listed, plain = forms(block_cases.PRODUCT_SEARCH, True), forms(block_cases.PRODUCT_LIST, True), forms(block_cases.PRODUCT_PLAIN, False)
+    assert len({f[1:] for f in search}) == 6 and [f[1:] for f in listed] == [f[1:] for f in search] == [f[1:] for f in plain]
+    assert {f[0] for f in search} == {1} and {f[0] for f in listed} == {2} and {f[0] for f in plain} == {1}
+
+
+def test_route_sizes_reach_both_forms(launches):
+    T = block_cases.ROUTE_TOKENS
+    def tokens_of_a_work_group(cases):
+        calls = [["smoe_route_scores", [T, E, k, 0, P, None, 0, None, 1, ng, tg, 1, None, 1, 1.0, P, P]] for E, ng, tg, k in cases]
+        return {-(-T // log[0][0]) for _, log in launches(calls)}
+    assert tokens_of_a_work_group(block_cases.ROUTE_PART_LANES) == {16} and tokens_of_a_work_group(block_cases.ROUTE_ODD_GROUPS) == {4}

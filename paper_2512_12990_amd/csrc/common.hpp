@@ -101,11 +101,8 @@ struct DeviceScope {
 };
 #define ON_DEVICE_OF(ctx) DeviceScope _scope((ctx)->device); HIPCHK(ctx, _scope.rc)
 
-// A grid of n work-groups of up to 1024 threads: a launch takes fewer than 2^32 threads along x, so from 2^20 work-groups on there are rows of 2^20.
-// row_group() counts them through; some of the last row may be too many.
-#define GRID_ROW_LOG 20
-static inline dim3 grid_of(unsigned n) { return n <= (1u << GRID_ROW_LOG) ? dim3(n) : dim3(1u << GRID_ROW_LOG, (n + (1u << GRID_ROW_LOG) - 1) >> GRID_ROW_LOG); }
-__device__ __forceinline__ int row_group() { return (int)((blockIdx.y << GRID_ROW_LOG) + blockIdx.x); }
+// A launch takes fewer than 2^32 threads along an axis: with a work-group of 1024 for every row, rows go in pieces of this many.
+#define ROWS_A_LAUNCH (1 << 20)
 
 static inline bool aligned16(const void* p) { return (((uintptr_t)p) & 15u) == 0; }
 

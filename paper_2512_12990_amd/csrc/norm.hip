@@ -7,6 +7,7 @@
 // written once.  Bound: HBM bytes with many rows, the launch and one memory round trip with few.  All arithmetic is
 // fp32; h' enters the second norm as it is before it is rounded to the residual's type.
 #include "common.hpp"
+#include <type_traits>
 
 struct NormArgs {
   const void* y; const float* slot_w; const void* post_w; const void* gate; const void* res; const void* pre_w;
@@ -31,9 +32,9 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float* red
 template <int ACT, int RES, int NT, int NC>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void residual_norm_kernel(NormArgs a) {
   __shared__ float red[2 * (NT / 64)];
-  const int t = NT == 64 ? row_group() * 4 + (threadIdx.x >> 6) : row_group();
+  const int t = NT == 64 ? (int)blockIdx.x * 4 + (threadIdx.x >> 6) : (int)blockIdx.x;
   const int tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
-  if (t >= a.T) return;                                 // (whole waves, and no barrier, or whole work-groups)
+  if (NT == 64 && t >= a.T) return;                     // (whole waves; no barrier in this form)
   const int d = a.d;
   const float inv_d = 1.0f / (float)d;
   const size_t row = (size_t)t * d;
@@ -117,14 +118,25 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void residual_norm_kernel(Norm
 }
 
 template <int ACT, int RES>
-static int launch_norm(smoe_ctx* ctx, const NormArgs& a) {
+static int launch_norm(smoe_ctx* ctx, NormArgs a) {
+  if (a.T > ROWS_A_LAUNCH) {
+    const size_t n = ROWS_A_LAUNCH, act = ACT == SMOE_F32 ? 4 : 2, res = RES == SMOE_F32 ? 4 : 2;
+    NormArgs rest = a;
+    a.T = ROWS_A_LAUNCH;
+    rest.T -= ROWS_A_LAUNCH;
+    auto skip = [](auto& p, size_t bytes) { if (p) p = (std::remove_reference_t<decltype(p)>)((uintptr_t)p + bytes); };
+    skip(rest.y, n * a.k * a.d * act); skip(rest.slot_w, n * a.k * 4); skip(rest.res, n * a.d * res); skip(rest.res_out, n * a.d * res); skip(rest.x_out, n * a.d * act);
+    if (a.gate_rows) skip(rest.gate, n * a.d * act);
+    if (const int rc = launch_norm<ACT, RES>(ctx, a)) return rc;
+    return launch_norm<ACT, RES>(ctx, rest);
+  }
   const int pieces = a.d / 8;
   hipStream_t st = ctx->stream;
-  if (pieces <= 64) residual_norm_kernel<ACT, RES, 64, 1><<<grid_of((a.T + 3) / 4), 256, 0, st>>>(a);
-  else if (pieces <= 256) residual_norm_kernel<ACT, RES, 256, 1><<<grid_of(a.T), 256, 0, st>>>(a);
-  else if (pieces <= 512) residual_norm_kernel<ACT, RES, 256, 2><<<grid_of(a.T), 256, 0, st>>>(a);
-  else if (pieces <= 1024) residual_norm_kernel<ACT, RES, 512, 2><<<grid_of(a.T), 512, 0, st>>>(a);
-  else residual_norm_kernel<ACT, RES, 1024, 2><<<grid_of(a.T), 1024, 0, st>>>(a);
+  if (pieces <= 64) residual_norm_kernel<ACT, RES, 64, 1><<<(a.T + 3) / 4, 256, 0, st>>>(a);
+  else if (pieces <= 256) residual_norm_kernel<ACT, RES, 256, 1><<<a.T, 256, 0, st>>>(a);
+  else if (pieces <= 512) residual_norm_kernel<ACT, RES, 256, 2><<<a.T, 256, 0, st>>>(a);
+  else if (pieces <= 1024) residual_norm_kernel<ACT, RES, 512, 2><<<a.T, 512, 0, st>>>(a);
+  else residual_norm_kernel<ACT, RES, 1024, 2><<<a.T, 1024, 0, st>>>(a);
   HIPCHK(ctx, hipGetLastError());
   return SMOE_OK;
 }

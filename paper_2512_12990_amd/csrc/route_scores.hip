@@ -315,8 +315,7 @@ __global__ __launch_bounds__(64 * SC_WAVES) void route_scores_long_kernel(ScoreA
 template <int ACT, int NT, int NJ>
 __global__ __launch_bounds__(RT_THREADS) void route_scores_x_kernel(ScoreArgs a, int T) {
   extern __shared__ __align__(16) uint8_t xdyn[];
-  const int E = a.r.E, t0 = row_group() * NT, nt = min(NT, T - t0);
-  if (nt <= 0) return;
+  const int E = a.r.E, t0 = (int)blockIdx.x * NT, nt = min(NT, T - t0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double* sel = (double*)xdyn;                                        // [NT][E]
   float* zt = (float*)(xdyn + (size_t)NT * E * 8);                    // [NT][E], then the activations
@@ -329,11 +328,19 @@ template <int ACT, int NT> static size_t scores_x_lds(int E, int d) { return (si
 
 template <int ACT, int NT>
 static int launch_scores_x(smoe_ctx* ctx, const ScoreArgs& a, int T) {
-  const int E = a.r.E;
-  const dim3 grid = grid_of((T + NT - 1) / NT);
+  const int E = a.r.E, grid = (T + NT - 1) / NT;
   const size_t lds = scores_x_lds<ACT, NT>(E, a.r.d_model);
   // half as many tokens per work-group where the activations of NT do not fit the LDS that a launch has without asking
   if constexpr (NT > 1) if (lds > 64u * 1024u) return launch_scores_x<ACT, NT / 2>(ctx, a, T);
+  if (T > ROWS_A_LAUNCH * NT) {
+    const size_t n = (size_t)ROWS_A_LAUNCH * NT;
+    ScoreArgs rest = a;
+    rest.r.x = (const uint8_t*)a.r.x + n * a.r.d_model * (ACT == SMOE_F32 ? 4 : 2);
+    rest.r.idx += n * a.r.k;
+    rest.r.w += n * a.r.k;
+    if (const int rc = launch_scores_x<ACT, NT>(ctx, a, (int)n)) return rc;
+    return launch_scores_x<ACT, NT>(ctx, rest, T - (int)n);
+  }
   if (E <= 64) route_scores_x_kernel<ACT, NT, 1><<<grid, RT_THREADS, lds, ctx->stream>>>(a, T);
   else route_scores_x_kernel<ACT, NT, 4><<<grid, RT_THREADS, lds, ctx->stream>>>(a, T);
   HIPCHK(ctx, hipGetLastError());

@@ -278,7 +278,8 @@ int smoe_prefill_histogram(smoe_ctx* ctx, const smoe_bank* routed, const smoe_ba
 /* T rows: b = sum_j slot_w[t,j] * y[t,j] over k slots (weights 1 if slot_w_dev is NULL); b = b / sqrt(mean(b^2) + eps) *
  * post_w unless post_w_dev is NULL; res_out = res + scale * gate * b; x_out = res_out / sqrt(mean(res_out^2) + eps) * pre_w.
  * y_dev [T,k,d], post_w_dev, pre_w_dev [d], gate_dev [d] or, with gate_rows = 1, [T,d], x_out_dev [T,d] of act_dtype;
- * slot_w_dev fp32 [T,k]; res_dev, res_out_dev [T,d] of res_dtype.  Everything is worked out in fp32, and x_out from res_out as it is
+ * slot_w_dev fp32 [T,k]; res_dev, res_out_dev [T,d] of res_dtype.  Everything is worked out in fp32 (so a row whose sum of squares leaves
+ * fp32's range, numbers of 1e17 to 1e19 and more by d, gives x_out 0; below some 1e-23 with eps 0 infinities), and x_out from res_out as it is
  * before its rounding.  NULL leaves a step out: gate_dev (1), pre_w_dev (1), res_dev (0), res_out_dev or x_out_dev (that
  * output is not written; one of them is needed), y_dev with k = 0 (the norm of a residual alone; slot_w_dev, post_w_dev
  * and gate_dev NULL then).  res_out_dev may be res_dev (in place); apart from that the outputs must not overlap the inputs
@@ -315,7 +316,7 @@ int smoe_mx_product_bytes(int T, int k, int E, int N, size_t* scratch_bytes);
 int smoe_mx_product(smoe_ctx* ctx, int E, int N, int K, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, int T,
                     int k, const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, int x_slots, const int32_t* idx_dev,
                     int swiglu, int out_dtype, void* scratch_dev, size_t scratch_bytes, void* y_dev);
-/* The same for decode steps of T <= 16 tokens, x_dev [T,K] or [T,k,K] of act_dtype taken as it is (not quantised),
+/* The same for decode steps of T <= 16 tokens (more have to be quantised, for smoe_mx_product), x_dev [T,K] or [T,k,K] of act_dtype taken as it is,
  * y_dev of act_dtype.  Every product of a weight and an activation is exact before the fp32 sum, but a weight of 2^128 or more
  * (possible with scale bytes 253 and 254) makes its sum infinite or NaN, and what an fp32 activation holds below 2^-133
  * counts as zero.  No scratch, one launch.  y_dev must not overlap x_dev. */

@@ -94,8 +94,9 @@ extern "C" int smoe_mx_dequantize(smoe_ctx* ctx, long long rows, int K, const ui
 //   A work-group takes 16 RT weight rows of one expert and up to 16 of the slots that chose this expert, so that every weight
 // byte is read once however many tokens share it.  Work-groups go by slots (that of a slot that is not the first of its expert has
 // nothing to do) or, with fewer experts than slots, by experts.  Its four or eight waves share the columns out, 128 at a time (32 columns of a row are one 16-byte load of a lane) and in turn,
-// so that the two halves of a line of weights are asked for together (a wave with neighbouring columns of its own: 30.2 against 27.9 us, 16 tokens, top-6 of 64, N 2048,
-// K 1408, fp32), and add their sums up through LDS.
+// so that the two halves of a line of weights are asked for together
+// (a wave with neighbouring columns of its own: 29.5 against 28.3 us in fp32, 23.3 against 21.5 in bf16; 16 tokens, top-6 of 64, N 2048, K 1408), and add their sums up through
+// LDS.  The figures here and below are microseconds a call in a captured graph that goes round over several layers' weights, so that these come from HBM.
 //   Codes are expanded to bf16, which holds e2m1 times a power of two exactly (below 2^128; infinite from there on), and multiplied by matrix instructions with
 // fp32 sums.  fp32 activations go in as three bf16 numbers whose sum they are (8 + 8 + 8 bits, cut off, not rounded), so
 // these products are exact too (bits below 2^-133, bf16's smallest, are cut off); the splitting is seven vector instructions a number, which is why it serves RT tiles of rows at once.
@@ -180,8 +181,9 @@ __global__ __launch_bounds__(64 * MV_WAVES) void mx_matvec_kernel(MatvecArgs a) 
   }
   const int units = (nb + 3) >> 2;
   // fp32 activations of so few slots that they fit are taken apart once for the whole work-group, [slot][part][units * 128], zeros behind the last block, else by
-  // every lane for itself.  Microseconds with / without (top-6 of 64, N 2048, K 1408): one token 7.1 / 8.4, 8 tokens 19.3 / 20.4, 16 tokens 29.5 / 30.1, where the
-  // work-groups of experts with three slots and more go on as long as before.
+  // every lane for itself.  Microseconds with / without (top-6 of 64, N 2048, K 1408): one token 7.2 / 7.5, 4 tokens 11.4 / 13.2, 8 tokens 19.6 / 20.7, 16 tokens
+  // 28.3 / 29.2, where the work-groups of experts with three slots and more go on as long as before.  Dense, K 2048: N 2048, one token 5.6 / 5.4, 4 tokens 6.0 / 5.6; N 8192, one token
+  // 9.1 / 10.2, 4 tokens 11.0 / 10.4; K and N 8192, one token 33.6 / 30.4.
   __bf16* split = (__bf16*)part;
   const int Kp = units * 128;
   const bool shared = PARTS > 1 && n_mine <= 16 && n_mine * Kp * PARTS * 2 <= (int)sizeof(part);
@@ -296,9 +298,12 @@ extern "C" int smoe_mx_matvec(smoe_ctx* ctx, int E, int N, int K, const uint8_t*
   ON_DEVICE_OF(ctx);
   const MatvecArgs a{w_codes_dev, w_scales_dev, x_dev, idx_dev, y_dev, E, N, K, T, k, x_slots, swiglu, T > 1 && E < T * k};
   // Rows of a work-group.  Four tiles share one fetch and one splitting of the activations between four waves, one unit of columns in flight each, so that many
-  // work-groups fit a CU; where that leaves too few work-groups, one tile and eight waves.  Microseconds with four tiles / with one: 16 tokens, top-6 of 64, N 2048,
-  // K 1408, fp32 29 / 65; 16 tokens, N 21888, K 2048, bf16 (342 work-groups) 13.7 / 18.4; 4 tokens, top-4 of 60, N 2816, K 2048 (704) 16.0 / 18.5; one token, top-6, the
-  // same matrices (264) 11.2 / 9.6; one token, dense, N 8192, K 8192 (128) 19.1 / 13.5, N 2048, K 10944 (32) 19.7 / 7.8; fp32, one token, top-6, N 2048, K 1408 (192) 7.3 / 7.7.
+  // work-groups fit a CU; where that leaves too few work-groups, one tile and eight waves.  Microseconds with four tiles / with one, K 2048, by work-groups of four:
+  //   fp32   dense 32: 16 tokens 10.9 / 7.4; dense 128: 1 token 9.2 / 8.7, 4 tokens 11.0 / 8.8, 16 tokens 11.9 / 12.3 (K 8192, 1 token: 33.7 / 24.1); dense 256: 1 token 10.0 / 14.7;
+  //          top-6 of 64, 264: 1 token 11.5 / 16.6; 2048 (K 1408): 16 tokens 28.6 / 64.5
+  //   bf16   dense 128: 16 tokens 8.9 / 8.3; dense 256: 1 token 8.6 / 8.6, 4 tokens 8.4 / 9.7, 16 tokens 9.4 / 13.6; dense 512: 1 token 11.9 / 14.4, 4 tokens 12.8 / 16.1;
+  //          top-6 of 64, 264: 1 token 10.9 / 9.3, 4 tokens 10.6 / 8.9; 528: 1 token 14.7 / 14.3; top-4 of 60, 704: 4 tokens 15.6 / 18.3; 2048 (K 1408): 16 tokens 21.9 / 32.8
+  // The limit in fp32 is somewhat low for long rows and few tokens, that of bf16 somewhat high for a dense matrix.
   const long long wgs = (long long)((N + 63) / 64) * (!idx_dev ? 1 : T * k < E ? T * k : E);
   if (act_dtype == SMOE_F32) {
     if (wgs < 128) launch_matvec<SMOE_F32, 1, 8>(ctx, a);

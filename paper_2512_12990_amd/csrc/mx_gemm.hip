@@ -120,8 +120,9 @@ __device__ __forceinline__ void to_lds4(u32x4 rsrc, uint32_t voff, uint32_t soff
 // pieces of a row are stored permuted (piece p at p ^ (row / 2 % 8)), so that sixteen lanes of an operand read, sixteen rows of
 // one piece, fall into different banks.  Half h of a wave multiplies blocks 4h .. 4h + 3 of a stage: its scales of
 // a row are one dword, a byte per step.
-//   What bounds it with many rows is the path from L2 to LDS: 33 - 38 bytes a cycle and CU in pieces of 128 bytes on whole lines with 64 to 96 KB on their way, 22 in pieces of
-// 64 bytes (half lines) or where rows do not begin on lines (K not a multiple of 256).
+//   What bounds it with many rows and long ones is the path from L2 to LDS: loads alone give 33 - 38 bytes a cycle and CU in pieces of 128 bytes on whole lines with 64 to 96 KB on
+// their way, 22 (0.34 lines) in pieces of 64 bytes or where rows do not begin on lines (K not a multiple of 256).  4096 x 2048 x 10944 asks for 0.27 - 0.29 lines a cycle and CU, start
+// and end counted in, with the matrix instructions busy a quarter of the time.
 //   Scales come 16 bytes a row at a time, two stages' worth: a dword per stage would cost as many requests to L2 as half the codes (dense product,
 // 4096 slots, N 2048, K 10944: 97 us with, 70 us without such loads).
 template <int NT, int NN, int FT, int FN> struct MgShape {
@@ -454,7 +455,7 @@ static const MxShape g_shapes[3] = {{32, 128, 2, 1.0}, {64, 128, 2, 1.34}, {128,
 static long long likely_tiles(int n, int E, int bt) { return E == 1 ? (n + bt - 1) / bt : n / bt + (n < E ? n : E + 1) / 2; }
 // The shape with the least rounds of work-groups times their cost; one round at least.  Microseconds of shapes 0 / 1 / 2 (top-6 of 64, N 2816, K 2048): 100
 // tokens 39.0 / 39.3 / 45.3, 300 47.2 / 44.4 / 53.1, 800 75.8 / 61.9 / 66.6, 1500 118 / 87.7 / 82.2; dense, N 2048, K 2048: 256 rows 6.1 / 7.5 / 11.7, 4096 28.2 / 21.0 / 16.9.
-static double rounds_of(const MxShape& s, int n, int E, int N) { return (double)likely_tiles(n, E, s.bt) * ((N + s.bn - 1) / s.bn) / (256.0 * s.per_cu); }      // (256 CUs)
+static double rounds_of(const MxShape& s, int n, int E, int N) { return (double)likely_tiles(n, E, s.bt) * ((N + s.bn - 1) / s.bn) / (256.0 * s.per_cu); }      // (256 CUs, whatever the device has: smoe_mx_product_bytes, which has to decide alike, knows no device)
 static int pick_shape(int n, int E, int N) {
   int best = 0;
   double least = 0.0;

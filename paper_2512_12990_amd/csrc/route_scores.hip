@@ -150,8 +150,9 @@ __device__ __forceinline__ void select_scores_wave(const ScoreArgs& a, int t, co
 // of a softmax: argument 1, exponential 2, divisor and product 2) and the sum with a bias below 4 by one of its own: two keys more than
 // 2^-20 max(1, |key|) apart are in order.  Logits more than 2^-30 apart, and where they decide
 // sigmoids at most 15, have binary64 scores that differ (slope of the sigmoid at 15: 3e-7).
-//   Bound: vector issue.  16384 tokens, 256 experts in 8 groups, top-8: 39 us with the long form alone, 28 with a short form of one token per wave, 22 with the pick
-// found by comparing and taken out by a mask (140 instructions a pick, now 50), 20 now, of which some 6 are the few tokens that need the long form.
+//   Bound: vector issue.  16384 tokens, 256 experts in 8 groups, top-8: 28 us with a short form of one token per wave, 22 with the pick found by comparing and taken
+// out by a mask (140 instructions a pick, now 50), 19.6 - 20.1 now, of which some 0.8 are the few tokens that need the long form (19.3 for logits far apart; 29.7 by the long
+// form alone).
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
 // the four steps of a reduction over a row of sixteen lanes: neighbour, neighbouring pair, other four of eight, other eight
 #define ROW_REDUCE(v, OP)      \
@@ -382,7 +383,14 @@ extern "C" int smoe_route_scores(smoe_ctx* ctx, int T, int E, int k, int d_model
     return launch_scores_x<SMOE_BF16, 8>(ctx, a, T);
   }
   // The short form needs rows of 16-byte pieces and groups of whole lanes, a power of two of them up to 8.  With few tokens its longer chain of
-  // instructions counts and not their number: 2047 tokens, 60 experts, top-4 5.4 us, by the long form 3.8; 16384, 256 experts, top-8 20 and 39.
+  // instructions counts and not their number.  Microseconds a call in a captured graph, short / long form, by tokens:
+  //                                             2048         2049         4096         8192          16384
+  //   60 experts, softmax, top-4             4.3 / 2.9    4.3 / 2.9    4.4 / 3.7    5.0 / 5.0     6.7 / 7.8
+  //   64 experts, sigmoid + bias, top-6      4.7 / 3.1    4.7 / 3.1    5.2 / 3.8    5.5 / 5.3     7.2 / 8.4
+  //   128 experts, softmax, top-8            6.1 / 5.4    6.1 / 6.0    6.2 / 7.4    7.3 / 11.6    11.5 / 20.2
+  //   256 experts, sigmoid + bias, top-8     9.0 / 5.6    9.0 / 6.1    9.2 / 7.6    10.8 / 12.3   17.1 / 21.9
+  //   256 in 8 groups, the same              11.1 / 7.3   11.0 / 8.1   11.2 / 9.9   13.0 / 16.5   19.6 / 29.7
+  // The switch at 2048 is right for 128 experts; with 64 and fewer the short form pays from some 8192 tokens on, with 256 from some 6000.
   const size_t lds = n_group > 1 ? (size_t)SC_WAVES * E * 8 : 0;
   const int nj = E <= 64 ? 4 : E <= 128 ? 8 : 16, lpg = E / n_group / nj;
   const bool brief = T > 2048 && E % 4 == 0 && (n_group == 1 || (E / n_group % nj == 0 && (lpg & (lpg - 1)) == 0));

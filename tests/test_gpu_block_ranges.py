@@ -55,14 +55,16 @@ def test_matvec_swiglu_far_below_zero(ctx, act):
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-def test_product_swiglu_far_below_zero(ctx, out):
-    """The same in the product of quantised numbers: a gate is the sum of codes times 16 and of codes times a half."""
+@pytest.mark.parametrize("T, N", [(72, 16), (1600, 2064), (4100, 2064)])
+def test_product_swiglu_far_below_zero(ctx, T, N, out):
+    """The same in the product of quantised numbers, in each tile shape: a gate is the sum of codes times 16 and of codes times a half.  With many rows three
+    in four have ordinary gates, next to them and in waves of their own."""
     grid = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])
     gates = [((4, 1, 0), (0, 0)), ((4, 1, .5), (0, 0)), ((4, 1.5, 0), (0, 0)), ((4, 1.5, 0), (1.5, 0)), ((4, 1.5, 0), (2, 0)), ((6, 0, 0), (0, 0)),
              ((6, 1.5, 0), (0, 0)), ((6, 3, 0), (1, 0)), ((6, 4, 1), (3, 0)), ((6, 6, 0), (0, 0)), ((6, 6, .5), (4, 1)), ((6, 6, 6), (0, 0))]
     ups = [(1, 127), (1.5, 127 + 30), (-6, 127 + 60), (3, 127 + 100), (-4, 127 + 120), (1, 127 - 60)]
     code = lambda v: int(np.nonzero(grid == abs(v))[0][0]) + (8 if v < 0 else 0)
-    N, K = 16, 96
+    K = 96
     wn = np.zeros((N, K), np.uint8)                          # codes, one a column
     wn[0::2, [0, 1, 2, 32, 33]] = 2
     wn[1::2, 64] = 2
@@ -75,11 +77,19 @@ def test_product_swiglu_far_below_zero(ctx, out):
             xs.append([131, 126, byte])
             g.append(-16.0 * sum(coarse) - 0.5 * sum(fine))
             u.append(v * 2.0 ** (byte - 127))
+    if T > 72:
+        at = np.random.default_rng(T).integers(0, len(g), size=T)
+        xn, xs, g, u = ([v[i] for i in at] for v in (xn, xs, g, u))
+        for t in range(T):
+            if t % 4 or t > T // 2:
+                xn[t] = xn[t].copy()
+                xn[t][:3] &= 8                               # gates of -4 and more
+                g[t] = -0.5 * sum(float(grid[n & 7]) for n in xn[t][32:34])
     pack = lambda n: np.ascontiguousarray(n[..., 0::2] | (n[..., 1::2] << 4))
     W = B.Mx(dev(pack(wn)), dev(np.full((N, 3), 127, np.uint8)))
     X = B.Mx(dev(pack(np.stack(xn))), dev(np.array(xs, np.uint8)))
     got = np64(B.smoe_mx_product(ctx, W, X, swiglu=True, out_dtype=DT[out]))[:, 0]
-    check_swiglu(got, np.array(g)[:, None] + np.zeros((1, 8)), np.array(u)[:, None] + np.zeros((1, 8)), out)
+    check_swiglu(got, np.array(g)[:, None] + np.zeros((1, N // 2)), np.array(u)[:, None] + np.zeros((1, N // 2)), out)
 
 
 # ------------------------------------------------------------------------------------ largest launches
